@@ -1,7 +1,8 @@
 """MI355X-native single pipeline stage of the offloading-based interleaved pipeline.
 
 The compute path is libstage.so (HIP kernels for gfx950 behind the C ABI of
-include/stage.h); ``stage`` is its ctypes binding with the same entry points.
+include/stage.h); ``stage`` is its ctypes binding with the same entry points, ``ops`` that of the
+operators on the caller's tensors (include/stage_ops.h).
 """
 from .stage import (  # noqa: F401
     StageConfig, StageLayerWeights, StageError, config_for, lib, EXPORTED, LIB_PATH,
@@ -17,4 +18,9 @@ from .stage import (  # noqa: F401
     stage_get_timeline, stage_set_timing, stage_get_stats, stage_strerror, stage_get_residency_log,
     stage_plan_offload, StagePlanInput, StagePlanStep, stage_allocate, StageAllocDevice, StageAllocInput,
     StageAllocPlan, STAGE_ALLOC_MAX_DEVICES, STAGE_ALLOC_MAX_LAYERS,
+    STAGE_F32, STAGE_BF16, STAGE_OPS_MAX_ROWS, STAGE_OPS_MAX_SEQS, STAGE_OPS_MAX_BLOCKS, STAGE_OPS_MAX_RANK,
+)
+from .ops import (  # noqa: F401
+    StageBatch, StageCache, StageAppendArgs, StageWindowArgs, StageAdapterArgs, stage_batch, stage_norm_rope_append,
+    stage_window_workspace, stage_window_attention, stage_adapter_workspace, stage_adapter_add,
 )

@@ -35,6 +35,7 @@
 #include <string>
 #include <vector>
 
+#include "device_guard.h"
 #include "stage.h"
 #include "stage_kernels.h"
 
@@ -205,18 +206,6 @@ struct stage {
     } while (0)
 
 namespace {
-
-struct DeviceGuard {
-    int prev = -1;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-        if (prev != dev) (void)hipSetDevice(dev);
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-    }
-};
 
 bool is_device_ptr(const void *p) {
     hipPointerAttribute_t attr;

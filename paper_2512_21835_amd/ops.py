@@ -1,0 +1,235 @@
+"""Binding of include/stage_ops.h: operators around a layer's projections, on torch tensors.
+
+Argument marshalling and the checks that need the tensors' shapes; the library checks the rest.  A call
+runs on the current torch stream of its tensors' device unless ``stream`` (a torch stream of it) is given,
+and returns the tensor that it writes.  Where a call needs a workspace and none is given, one is taken
+from torch's allocator, on that stream.
+"""
+from __future__ import annotations
+
+import ctypes
+from ctypes import c_float, c_int32, c_int64, c_void_p
+from typing import Optional, Sequence
+
+import torch
+
+from .stage import STAGE_BF16, STAGE_F32, _check, lib
+
+_TYPES = {torch.float32: STAGE_F32, torch.bfloat16: STAGE_BF16}
+
+
+class StageBatch(ctypes.Structure):
+    """stage_batch of include/stage_ops.h; stage_batch() makes one and keeps its tensors."""
+    _fields_ = [("n_seqs", c_int32), ("max_rows", c_int32), ("max_len", c_int32), ("max_blocks", c_int32),
+                ("row_start", c_void_p), ("length", c_void_p), ("block_table", c_void_p)]
+
+
+class StageCache(ctypes.Structure):
+    _fields_ = [("pool", c_void_p), ("n_blocks", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32),
+                ("type", c_int32)]
+
+
+class StageAppendArgs(ctypes.Structure):
+    _fields_ = [("device", c_int32), ("batch", StageBatch), ("cache", StageCache), ("rows", c_int32),
+                ("n_q_heads", c_int32), ("qkv", c_void_p), ("q_out", c_void_p), ("qkv_ld", c_int64), ("q_ld", c_int64),
+                ("qkv_type", c_int32), ("q_type", c_int32), ("q_gain", c_void_p), ("k_gain", c_void_p),
+                ("eps", c_float), ("n_angles", c_int32), ("cos", c_void_p), ("sin", c_void_p),
+                ("positions", c_void_p), ("n_axes", c_int32), ("section", c_int32 * 3)]
+
+
+class StageWindowArgs(ctypes.Structure):
+    _fields_ = [("device", c_int32), ("batch", StageBatch), ("cache", StageCache), ("rows", c_int32),
+                ("n_q_heads", c_int32), ("window", c_int32), ("sinks", c_int32), ("scale", c_float), ("q", c_void_p),
+                ("out", c_void_p), ("q_ld", c_int64), ("out_ld", c_int64), ("type", c_int32)]
+
+
+class StageAdapterArgs(ctypes.Structure):
+    _fields_ = [("device", c_int32), ("rows", c_int32), ("k", c_int32), ("n", c_int32), ("n_adapters", c_int32),
+                ("max_rank", c_int32), ("type", c_int32), ("x", c_void_p), ("base", c_void_p), ("out", c_void_p),
+                ("x_ld", c_int64), ("base_ld", c_int64), ("out_ld", c_int64), ("a", c_void_p), ("b", c_void_p),
+                ("ids", c_void_p), ("ranks", c_void_p), ("scales", c_void_p)]
+
+
+def _device(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a GPU")
+    return t.device.index
+
+
+def _type(t: torch.Tensor) -> int:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"float32 or bfloat16 is needed, got {t.dtype}")
+    return kind
+
+
+def _plain(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: Sequence[int], device: int) -> Optional[int]:
+    """Address of a contiguous tensor of this type, shape (None: any) and device; None for none."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or _device(t) != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {len(shape)} dimensions on the call's device")
+    for have, want in zip(t.shape, shape):
+        if want is not None and have != want:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is needed")
+    return t.data_ptr()
+
+
+def _row_stride(t: torch.Tensor, name: str, device: int) -> int:
+    """Elements from row to row of [rows, width] or [rows, heads, head_dim], whose rows are each contiguous."""
+    shape, stride = t.shape, t.stride()
+    if _device(t) != device:
+        raise ValueError(f"{name} is on another device")
+    width = 1
+    for n, s in zip(reversed(shape[1:]), reversed(stride[1:])):
+        if n != 1 and s != width:
+            raise ValueError(f"the rows of {name} must be contiguous")
+        width *= n
+    return stride[0] if shape[0] > 1 else width
+
+
+def _cache(pool: torch.Tensor, device: int) -> StageCache:
+    if pool.dim() != 5 or pool.shape[1] != 2 or pool.shape[3] != 16 or not pool.is_contiguous() or _device(pool) != device:
+        raise ValueError("pool must be a contiguous tensor [n_blocks, 2, n_kv_heads, 16, head_dim] on the call's device")
+    return StageCache(pool.data_ptr(), pool.shape[0], pool.shape[2], pool.shape[4], _type(pool))
+
+
+def _batch(batch: StageBatch, device: int) -> StageBatch:
+    if batch.device != device:
+        raise ValueError("the batch is on another device")
+    return batch
+
+
+def _workspace(size, args, device: int, given: Optional[torch.Tensor], stream):
+    """The workspace tensor of a call (None: it takes none)."""
+    if given is not None:
+        if not given.is_contiguous() or _device(given) != device:
+            raise ValueError("the workspace must be a contiguous tensor on the call's device")
+        return given
+    need = c_int64()
+    _check(size(ctypes.byref(args), ctypes.byref(need)))
+    if need.value == 0:
+        return None
+    if stream is None:
+        return torch.empty(need.value, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(need.value, dtype=torch.uint8, device=device)
+
+
+def _handle(stream, device: int) -> int:
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device.index != device:
+        raise ValueError("the stream is on another device")
+    return stream.cuda_stream
+
+
+def stage_batch(row_start: torch.Tensor, length: torch.Tensor, block_table: torch.Tensor, max_rows: int,
+                max_len: int) -> StageBatch:
+    """The sequences of a call: int32 row_start [n + 1], length [n] and block_table [n, max_blocks]; no sequence
+    has more than max_rows rows or holds more than max_len tokens."""
+    device, n = _device(row_start), length.shape[0]
+    b = StageBatch(n, max_rows, max_len, block_table.shape[-1], _plain(row_start, "row_start", torch.int32, (n + 1,), device),
+                   _plain(length, "length", torch.int32, (n,), device),
+                   _plain(block_table, "block_table", torch.int32, (n, None), device))
+    b.device, b.tensors = device, (row_start, length, block_table)
+    return b
+
+
+def stage_norm_rope_append(qkv: torch.Tensor, q_out: torch.Tensor, pool: torch.Tensor, batch: StageBatch,
+                           cos: torch.Tensor, sin: torch.Tensor, q_gain: Optional[torch.Tensor] = None,
+                           k_gain: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                           positions: Optional[torch.Tensor] = None, sections: Optional[Sequence[int]] = None,
+                           stream=None) -> torch.Tensor:
+    """Norm of the query and key heads of qkv [rows, Hq + 2 Hkv, d], rotation, append to pool; queries to q_out [rows, Hq,
+    d].  positions int32 [rows], or [3, rows] with the pairs per axis in ``sections``."""
+    device = _device(qkv)
+    cache = _cache(pool, device)
+    d, hkv = cache.head_dim, cache.n_kv_heads
+    if qkv.dim() != 3 or q_out.dim() != 3 or qkv.shape[2] != d or q_out.shape[2] != d or q_out.shape[0] != qkv.shape[0] or \
+            qkv.shape[1] != q_out.shape[1] + 2 * hkv:
+        raise ValueError(f"qkv {tuple(qkv.shape)}, q_out {tuple(q_out.shape)} and pool {tuple(pool.shape)} do not fit")
+    rows, axes = qkv.shape[0], 1 if positions is None or positions.dim() == 1 else 3
+    if positions is not None and (axes == 3) != (sections is not None):
+        raise ValueError("positions of three axes come with the pairs of each in sections")
+    if sections is not None and (positions is None or len(sections) != 3):
+        raise ValueError("sections are three numbers, and come with positions [3, rows]")
+    args = StageAppendArgs(
+        device, _batch(batch, device), cache, rows, q_out.shape[1], qkv.data_ptr(), q_out.data_ptr(),
+        _row_stride(qkv, "qkv", device), _row_stride(q_out, "q_out", device), _type(qkv), _type(q_out),
+        _plain(q_gain, "q_gain", torch.bfloat16, (d,), device), _plain(k_gain, "k_gain", torch.bfloat16, (d,), device),
+        eps, cos.shape[0], _plain(cos, "cos", torch.float32, (None, d // 2), device),
+        _plain(sin, "sin", torch.float32, (cos.shape[0], d // 2), device),
+        _plain(positions, "positions", torch.int32, (rows,) if axes == 1 else (3, rows), device), axes,
+        (c_int32 * 3)(*(sections or (d // 2, 0, 0))))
+    if rows:
+        _check(lib().stage_norm_rope_append(ctypes.byref(args), _handle(stream, device)))
+    return q_out
+
+
+def _window_args(q, out, pool, batch, window, sinks, scale):
+    device = _device(q)
+    cache = _cache(pool, device)
+    if q.dim() != 3 or q.shape != out.shape or q.dtype != out.dtype or q.shape[2] != cache.head_dim:
+        raise ValueError(f"q {tuple(q.shape)} {q.dtype}, out {tuple(out.shape)} {out.dtype} and pool {tuple(pool.shape)} do not fit")
+    return device, StageWindowArgs(device, _batch(batch, device), cache, q.shape[0], q.shape[1], window, sinks, scale,
+                                   q.data_ptr(), out.data_ptr(), _row_stride(q, "q", device),
+                                   _row_stride(out, "out", device), _type(q))
+
+
+def stage_window_workspace(q: torch.Tensor, out: torch.Tensor, pool: torch.Tensor, batch: StageBatch, window: int = 0,
+                           sinks: int = 0) -> int:
+    """Bytes of workspace that stage_window_attention takes with these arguments."""
+    need = c_int64()
+    _check(lib().stage_window_workspace(ctypes.byref(_window_args(q, out, pool, batch, window, sinks, 0.0)[1]), ctypes.byref(need)))
+    return need.value
+
+
+def stage_window_attention(q: torch.Tensor, out: torch.Tensor, pool: torch.Tensor, batch: StageBatch, window: int = 0,
+                           sinks: int = 0, scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
+                           stream=None) -> torch.Tensor:
+    """Attention of q [rows, Hq, d] over pool: positions of the last ``window`` tokens (0: all) and the first ``sinks``."""
+    device, args = _window_args(q, out, pool, batch, window, sinks, scale)
+    if q.shape[0]:
+        L = lib()
+        ws = _workspace(L.stage_window_workspace, args, device, workspace, stream)
+        _check(L.stage_window_attention(ctypes.byref(args), None if ws is None else ws.data_ptr(),
+                                        0 if ws is None else ws.nbytes, _handle(stream, device)))
+    return out
+
+
+def _adapter_args(x, base, out, a, b, ids, ranks, scales):
+    device = _device(x)
+    if x.dim() != 2 or base.dim() != 2 or base.shape != out.shape or base.shape[0] != x.shape[0] or \
+            not x.dtype == base.dtype == out.dtype or a.dim() != 3:
+        raise ValueError(f"x {tuple(x.shape)} {x.dtype}, base {tuple(base.shape)} {base.dtype} and out {tuple(out.shape)} "
+                         f"{out.dtype} do not fit")
+    (rows, k), n, (count, rank) = x.shape, base.shape[1], a.shape[:2]
+    return device, StageAdapterArgs(
+        device, rows, k, n, count, rank, _type(x), x.data_ptr(), base.data_ptr(), out.data_ptr(),
+        _row_stride(x, "x", device), _row_stride(base, "base", device), _row_stride(out, "out", device),
+        _plain(a, "a", torch.bfloat16, (count, rank, k), device), _plain(b, "b", torch.bfloat16, (count, n, rank), device),
+        _plain(ids, "ids", torch.int32, (rows,), device), _plain(ranks, "ranks", torch.int32, (count,), device),
+        _plain(scales, "scales", torch.float32, (count,), device))
+
+
+def stage_adapter_workspace(x, base, out, a, b, ids, ranks=None, scales=None) -> int:
+    """Bytes of workspace that stage_adapter_add takes with these arguments."""
+    need = c_int64()
+    args = _adapter_args(x, base, out, a, b, ids, ranks, scales)[1]
+    _check(lib().stage_adapter_workspace(ctypes.byref(args), ctypes.byref(need)))
+    return need.value
+
+
+def stage_adapter_add(x: torch.Tensor, base: torch.Tensor, out: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                      ids: torch.Tensor, ranks: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out [rows, n] = base + scales[i] * b[i] (a[i] x), i = ids of the row: x [rows, k], a [n_adapters, max_rank, k], b
+    [n_adapters, n, max_rank]; ids out of range: no adapter."""
+    device, args = _adapter_args(x, base, out, a, b, ids, ranks, scales)
+    if x.shape[0]:
+        L = lib()
+        ws = _workspace(L.stage_adapter_workspace, args, device, workspace, stream)
+        _check(L.stage_adapter_add(ctypes.byref(args), None if ws is None else ws.data_ptr(),
+                                   0 if ws is None else ws.nbytes, _handle(stream, device)))
+    return out

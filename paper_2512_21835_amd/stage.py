@@ -38,7 +38,13 @@ EXPORTED = (
     "stage_get_demotion_log", "stage_get_residency_log", "stage_get_timeline", "stage_set_timing", "stage_get_stats",
     "stage_last_error", "stage_strerror", "stage_plan_offload", "stage_allocate", "stage_kv_park", "stage_kv_unpark",
     "stage_decode_noalloc",
+    "stage_norm_rope_append", "stage_window_workspace", "stage_window_attention", "stage_adapter_workspace",
+    "stage_adapter_add",
 )
+STAGE_F32, STAGE_BF16 = 0, 1
+STAGE_OPS_MAX_ROWS = STAGE_OPS_MAX_BLOCKS = 1048576
+STAGE_OPS_MAX_SEQS = 65536
+STAGE_OPS_MAX_RANK = 256
 STAGE_NOALLOC_SCRATCH_BYTES = 67108864
 STAGE_ALLOC_MAX_DEVICES = 64
 STAGE_ALLOC_MAX_LAYERS = 4096
@@ -143,6 +149,11 @@ def lib():
         "stage_get_stats": (c_int32, [c_void_p, c_char_p, c_int32]),
         "stage_last_error": (c_char_p, [c_void_p]),
         "stage_strerror": (c_char_p, [c_int32]),
+        "stage_norm_rope_append": (c_int32, [c_void_p, c_void_p]),
+        "stage_window_workspace": (c_int32, [c_void_p, c_void_p]),
+        "stage_window_attention": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p]),
+        "stage_adapter_workspace": (c_int32, [c_void_p, c_void_p]),
+        "stage_adapter_add": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
