@@ -50,7 +50,7 @@ OpRows op_rows(const stage_batch &b, const stage_cache &c, int rows) {
     r.length = b.length;
     r.table = b.block_table;
     r.n_seqs = b.n_seqs;
-    r.max_rows = b.max_rows;
+    r.max_rows = b.max_rows < rows ? b.max_rows : rows;
     r.max_len = b.max_len;
     r.max_blocks = b.max_blocks;
     r.rows = rows;
