@@ -113,7 +113,7 @@ typedef struct {
     int32_t n_q_heads; /* n_kv_heads times 1, 2, 4 or 8 */
     int32_t window;    /* >= 0; 0: no window */
     int32_t sinks;     /* >= 0 */
-    float scale;       /* 0: 1 / sqrt(head_dim) */
+    float scale;       /* 0: 1 / sqrt(head_dim); else of a size from 1e-30 to 1e30 */
     const void *q;     /* [rows, q_ld >= n_q_heads head_dim] */
     void *out;         /* [rows, out_ld >= n_q_heads head_dim] */
     int64_t q_ld, out_ld;

@@ -65,7 +65,7 @@ int status(hipError_t e) {
 
 bool window_sizes(const stage_window_args &a) {
     return sizes_ok(a.batch, a.cache, a.rows, a.n_q_heads) && a.window >= 0 && a.sinks >= 0 && is_type(a.type) &&
-           std::isfinite(a.scale);
+           (a.scale == 0.f || (std::fabs(a.scale) >= 1e-30f && std::fabs(a.scale) <= 1e30f));
 }
 
 WindowArgs window_args(const stage_window_args &a, void *workspace) {

@@ -6,10 +6,11 @@
 //
 // window_split: rows in blocks of 16 columns (G query heads of a KV head x 16 / G positions), the pages cut
 // over workgroups and their wavefronts, states joined at the end (window_merge where the workgroups are several).
+#include <type_traits>
+
 #include "lanes.h"
 #include "lds_dma.h"
 #include "ops_kernels.h"
-#include "pair.h"
 #include "stage_ops.h"
 
 namespace stg {
@@ -17,7 +18,9 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef const __attribute__((address_space(4))) int *const_ints;
 typedef __attribute__((address_space(3))) u32x4 *lds16;
@@ -26,6 +29,15 @@ typedef __attribute__((address_space(3))) float *lds4;
 
 constexpr int kPage = kBlockTokens;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;
+
+// The same in every lane, and known to be.
+__device__ __forceinline__ OpRows::Seq uniform(OpRows::Seq s) {
+    const uint64_t t = (uint64_t)(uintptr_t)s.table;
+    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)t), high = __builtin_amdgcn_readfirstlane((uint32_t)(t >> 32));
+    return {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.pos0),
+            reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low))};
+}
 
 // The pages that rows at positions first .. last see: pages 0 .. sink - 1, then from, from + 1, ...; n in all.
 struct Span {
@@ -43,7 +55,7 @@ __device__ __forceinline__ Span span_of(const WindowArgs &a, int first, int last
     return s;
 }
 __device__ __forceinline__ bool sees(const WindowArgs &a, int pos, int key) {
-    return key <= pos && key < a.rows.max_len && (key > pos - a.window || key < a.sinks);
+    return (key <= pos) & (key < a.rows.max_len) & ((key > pos - a.window) | (key < a.sinks));   // (no branches)
 }
 // Whether rows at positions first .. last all see keys k0 .. k0 + n - 1.
 __device__ __forceinline__ bool all_see(const WindowArgs &a, int first, int last, int k0, int n) {
@@ -74,8 +86,8 @@ __device__ __forceinline__ void store4(void *p, size_t e, int type, float4 v) {
 }
 // o / l; a row that saw no key is 0.
 __device__ __forceinline__ float4 quotient(float4 o, float l) {
-    if (l == 0.f) return make_float4(0.f, 0.f, 0.f, 0.f);
-    return make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    return make_float4(o.x * r, o.y * r, o.z * r, o.w * r);
 }
 
 // Term t of x as a sum of bf16 terms, each the nearest to what the ones before leave: three terms hold all 24 bits.
@@ -120,6 +132,11 @@ struct Columns {
     int pos;          // of the column's row; -1: no row
 
     __device__ __forceinline__ void init(const WindowArgs &a, size_t q_at, bool valid) {
+        if (a.type == STAGE_F32) init_of<STAGE_F32>(a, q_at, valid);
+        else init_of<STAGE_BF16>(a, q_at, valid);
+    }
+    template <int TYPE>
+    __device__ __forceinline__ void init_of(const WindowArgs &a, size_t q_at, bool valid) {
         const int lane = __lane_id(), lq = lane >> 4;
         m = -INFINITY;
         l = 0.f;
@@ -129,7 +146,7 @@ struct Columns {
 #pragma unroll
             for (int v = 0; v < D / 16; ++v) {
                 float x[4] = {0.f, 0.f, 0.f, 0.f};
-                if (valid) load4(a.q, q_at + 16 * v + 4 * lq, a.type, x);
+                if (valid) load4(a.q, q_at + 16 * v + 4 * lq, TYPE, x);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) qf[4 * v + c] = x[c];
             }
@@ -138,8 +155,8 @@ struct Columns {
             for (int s = 0; s < D / 32; ++s) {
                 float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                 if (valid) {
-                    load4(a.q, q_at + 32 * s + 8 * lq, a.type, x);
-                    load4(a.q, q_at + 32 * s + 8 * lq + 4, a.type, x + 4);
+                    load4(a.q, q_at + 32 * s + 8 * lq, TYPE, x);
+                    load4(a.q, q_at + 32 * s + 8 * lq + 4, TYPE, x + 4);
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -184,7 +201,7 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             p[i] = (sc[i] + s1[i]) * scale;
-            if (masked && !sees(a, pos, k0 + 4 * lq + i)) p[i] = -INFINITY;
+            p[i] = !masked | sees(a, pos, k0 + 4 * lq + i) ? p[i] : -INFINITY;
             top = fmaxf(top, p[i]);
         }
         top = fmaxf(top, lane_xor(top, 16));
@@ -250,7 +267,7 @@ struct Columns {
         for (int c = 0; c < N; ++c) {
             const int at = 64 * c + lane, key = k0 + at / L::CH;
             // (a key between two rows' windows is in one of them: the rows are neighbours)
-            if (!sees(a, last, key) && !(key <= last && sees(a, max(first, key), key))) {
+            if (!(sees(a, last, key) | ((key <= last) & sees(a, max(first, key), key)))) {
                 *(lds16)(vr + 16 * at) = u32x4{0, 0, 0, 0};
             } else if (rows > 1) {
                 u32x4 v = *(lds16)(vr + 16 * at);
@@ -318,7 +335,7 @@ __global__ __launch_bounds__(256) void window_split(WindowArgs a, SplitPlan pl) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, block = blockIdx.x / hkv, split = blockIdx.y;
     const int bq = 16 >> pl.log_g, seq_i = block / pl.blocks_per_seq, t0 = block % pl.blocks_per_seq * bq;
-    const OpRows::Seq seq = a.rows.seq(seq_i);
+    const OpRows::Seq seq = uniform(a.rows.seq(seq_i));
     const int n = min(seq.n, a.rows.max_rows);
     if (t0 >= n) return;
     const int rows = min(bq, n - t0), first = seq.pos0 + t0, last = first + rows - 1;
@@ -494,10 +511,413 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Prompts.  A workgroup: 128 CB columns = G heads x BQ = 128 CB / G consecutive rows of one sequence, one KV head; wavefront
+// w the columns 32 CB w .. (column r: head r / BQ, row r % BQ).  K and V tiles of 32 keys (two pages) go straight into
+// a ring of LDS stages, one barrier per tile.  S^T = K Q^T: lane l holds keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for
+// column l % 32, the k order of the operand P^T of O^T += V^T P^T; 32x32x16 MFMAs, q and p as TERMS bf16 terms.
+//
+// In turn t a wavefront multiplies tile t + 1's K by Q and tile t - 1's V by P while it takes the softmax of
+// tile t: the three are independent, and the vector instructions of the softmax (as long as the MFMAs with one
+// term) are laid between the MFMAs by hand.
+template <int D, int CB>
+struct TileLds {
+    static constexpr int KEYS = 32, ROW = 2 * D, HALF = KEYS * ROW, BYTES = 2 * HALF, CH = ROW / 16;
+    // tile t - 1 is read until the end of turn t: its stage takes tile t + S - 1 in turn t + 1
+    static constexpr int STAGES = CB == 1 && D == 128 ? 5 : 6;
+    static constexpr int KPC = 1024 / ROW, COPIES = 8 / KPC;   // keys per copy; copies of K (and of V) per wavefront
+    __device__ static int kx(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
+    __device__ static int vx(int key) { return D == 128 ? (key & 3) << 2 : (key & 2) << 1; }
+};
+
+// Clears the elements of eight bf16 that are not finite; whether there are any.
+__device__ __forceinline__ bool clear_odd(u32x4 &v) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t bad = ((v[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;   // exponents all ones
+        odd |= bad;
+        v[j] &= ~((bad >> 15) * 0xFFFFu);
+    }
+    return odd != 0;
+}
+
+struct TilePlan {
+    int log_g;
+};
+
+template <int D, int TERMS, int CB>
+__global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_tiles(WindowArgs a, TilePlan pl) {
+    using L = TileLds<D, CB>;
+    constexpr int S = L::STAGES, KK = D / 16, NB = D / 32, KT = L::KEYS;
+    constexpr int TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32;   // of q and out
+    __shared__ __align__(1024) char lds[S * L::BYTES];
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, log_bq = (CB == 1 ? 7 : 8) - pl.log_g, bq = 1 << log_bq;
+    // the sequence and the block of its rows: blocks of all sequences in turn
+    int block = blockIdx.x / hkv, seq_i = 0;
+    for (;; seq_i += 64) {
+        if (seq_i >= a.rows.n_seqs) return;
+        const int i = seq_i + lane;
+        const int own = i < a.rows.n_seqs ? (min(a.rows.seq(i).n, a.rows.max_rows) + bq - 1) >> log_bq : 0;
+        int sum = own;
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) {
+            const int v = __shfl_up(sum, x, 64);
+            if (lane >= x) sum += v;
+        }
+        const int before = __popcll(__builtin_amdgcn_ballot_w64(sum <= block));   // (sums ascend)
+        if (before < 64) {
+            const int skipped = __builtin_amdgcn_readlane(sum - own, before), mine = __builtin_amdgcn_readlane(own, before);
+            block = mine - 1 - (block - skipped);      // the last rows, which see the most keys, first
+            seq_i += before;
+            break;
+        }
+        block -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    const OpRows::Seq seq = uniform(a.rows.seq(__builtin_amdgcn_readfirstlane(seq_i)));
+    const int t0 = __builtin_amdgcn_readfirstlane(block) << log_bq, rows = min(bq, min(seq.n, a.rows.max_rows) - t0), first = seq.pos0 + t0;
+    // the tiles that some row sees: 0 .. sink - 1, then from, from + 1, ...
+    const int end = min(first + rows, a.rows.max_len), last_page = max(end - 1, 0) / kPage;
+    const int sink = (max(0, min(a.sinks, end)) + KT - 1) / KT, from = max(max(0, first - a.window + 1) / KT, sink);
+    const int n_tiles = end <= 0 ? 0 : sink + max(0, (end + KT - 1) / KT - from);
+    auto tile_at = [&](int t) { return t < sink ? t : from + t - sink; };
+
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const size_t head = (size_t)kPage * L::ROW, block_bytes = (size_t)2 * hkv * head;
+    const char *const pool = static_cast<const char *>(a.pool) + g * head;
+    auto known = [&](int b) { return (unsigned)b < (unsigned)a.rows.n_blocks; };
+    struct Pages { int b[2]; };
+    auto pages_of = [&](int t) {
+        const int p = 2 * tile_at(t);
+        const_ints table = (const_ints)(uintptr_t)seq.table;
+        return Pages{{table[min(p, last_page)], table[min(p + 1, last_page)]}};
+    };
+    // the wavefront's share of a tile: 8 keys of K and of V, of one page
+    auto copy = [&](int t, const Pages &pg) {
+        const int b = wave < 2 ? pg.b[0] : pg.b[1];
+        const char *const k = pool + (size_t)(known(b) ? b : 0) * block_bytes + (wave & 1) * 8 * L::ROW;
+        const uint32_t st = ring + t % S * L::BYTES + 8 * wave * L::ROW;
+        const int r = lane / L::CH, c = lane % L::CH;
+#pragma unroll
+        for (int i = 0; i < L::COPIES; ++i) {
+            const int key = L::KPC * i + r, row = 8 * wave + key;
+            dma16(key * L::ROW + 16 * (c ^ L::kx(row)), k, st + 1024 * i);
+            dma16(key * L::ROW + 16 * (c ^ L::vx(row)), k + hkv * head, st + L::HALF + 1024 * i);
+        }
+    };
+    Pages pg[S];   // of tiles t, t + 1, ...
+#pragma unroll
+    for (int i = 0; i < S; ++i) pg[i] = i < n_tiles ? pages_of(i) : Pages{{-1, -1}};
+#pragma unroll
+    for (int i = 0; i < S - 2; ++i)
+        if (i < n_tiles) copy(i, pg[i]);
+
+    // the wavefront's columns and the rows that they have: positions w_first .. w_last
+    const int c0 = 32 * CB * wave, r0 = bq >= 32 * CB ? c0 & (bq - 1) : 0;
+    const int w_rows = min(bq >= 32 * CB ? 32 * CB : bq, rows - r0), w_first = first + r0, w_last = w_first + w_rows - 1;
+    bf16x8_t q[CB][TERMS][KK];
+    f32x16_t o[CB][NB];
+    float m[CB], l[CB];
+    int pos[CB];
+    size_t q_at[CB];
+#pragma unroll
+    for (int x = 0; x < CB; ++x) {
+        const int r = c0 + 32 * x + col, t = r & (bq - 1);
+        pos[x] = t < rows ? first + t : -1;
+        m[x] = -INFINITY;
+        l[x] = 0.f;
+        q_at[x] = (size_t)(seq.first + t0 + min(t, rows - 1)) * a.q_ld + (size_t)((g << pl.log_g) + (r >> log_bq)) * D + 8 * half;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            float v[8];
+            load4(a.q, q_at[x] + 16 * kk, TYPE, v);
+            load4(a.q, q_at[x] + 16 * kk + 4, TYPE, v + 4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                __bf16 s[TERMS];
+                split_terms<TERMS>(a.scale < 0.f ? -v[j] : v[j], s);   // (its scores' maximum is then the largest)
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) q[x][i][kk][j] = s[i];
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[x][b][i] = 0.f;
+    }
+    bool odd = false;
+    const float scale = fabsf(a.scale) * kLog2e;   // scores in base 2
+    const uint32_t k_at = ring + col * L::ROW + 16 * (half ^ L::kx(col));   // chunk 2 kk + half of key col, permuted
+    const int vk = 4 * half + (lane & 15) / 4;
+    const uint32_t v_at = ring + L::HALF + vk * L::ROW + 8 * (lane & 1) + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ L::vx(vk));
+    auto stage = [&](int t) { return (uint32_t)(t % S * L::BYTES); };
+    auto both_known = [&](const Pages &p) { return known(p.b[0]) & known(p.b[1]); };
+    // (wave-uniform) whether some row of the wavefront sees a key of tile t
+    auto active = [&](int t) {
+        const int k0 = tile_at(t) * KT;
+        return (t >= 0) & (t < n_tiles) & (w_rows > 0) & (k0 <= w_last) & ((k0 < a.sinks) | (k0 + KT - 1 > w_first - a.window));
+    };
+    // This wavefront's share of tile t has landed; with the barrier behind it, everybody's.  In a tile that not every
+    // row sees, a V that is not finite must not meet the matrix instructions (0 x inf): it becomes 0 here, and is
+    // added at the end for the columns that see it.
+    auto landed = [&](int t, int behind, const Pages &p) {   // behind: tiles under way behind it
+        if (S > 5 && behind >= 2) wait_vm<(S > 5 ? 2 : 1) * 2 * L::COPIES>();
+        else if (S > 4 && behind >= 1) wait_vm<2 * L::COPIES>();
+        else wait_vm<0>();
+        asm volatile("" ::: "memory");
+        if (t < n_tiles && !(all_see(a, first, first + rows - 1, tile_at(t) * KT, KT) & both_known(p))) {
+            const uint32_t at = ring + stage(t) + L::HALF + 8 * wave * L::ROW + 16 * lane;
+#pragma unroll
+            for (int i = 0; i < L::COPIES; ++i) {
+                u32x4 v = *(lds16)(at + 1024 * i);
+                const bool bad = clear_odd(v);
+                odd |= bad;
+                if (bad) *(lds16)(at + 1024 * i) = v;
+            }
+        }
+    };
+    auto hide = [&](f32x16_t(&s)[CB], int t, const Pages &p) {
+        const int k0 = tile_at(t) * KT;
+        const bool now = active(t), k1 = known(p.b[0]), k2 = known(p.b[1]);
+#pragma unroll
+        for (int x = 0; x < CB; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool seen = sees(a, pos[x], k0 + 8 * (i / 4) + 4 * half + i % 4) & (i < 8 ? k1 : k2) & now;
+                s[x][i] = seen ? s[x][i] : -INFINITY;
+            }
+    };
+    auto key_frag = [&](uint32_t k, int kk) { return __builtin_bit_cast(bf16x8_t, *(lds16)(k ^ (32 * kk))); };
+    auto value_frag = [&](uint32_t v, int h, int b) {
+        const uint32_t at = (v ^ (64 * b)) + 16 * h * L::ROW;
+        const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)at);
+        const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)(at + 8 * L::ROW));
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // The maximum that scores are taken relative to: a whole number (so that rescaling is exact, what is already
+    // rounded to bf16 included) which stays until a score is 2^kSlack beyond it: p and its sums are floating
+    // point, and the rescaling, a quarter of a tile's vector work, is rare after the first tile.
+    auto raise = [&](const float(&top)[CB], bf16x8_t(&p)[CB][TERMS][2]) {
+#pragma unroll
+        for (int x = 0; x < CB; ++x) {
+            const float best = fmaxf(top[x], lane_xor(top[x], 32)) * scale;
+            if (__builtin_amdgcn_ballot_w64(best > m[x] + kSlack) == 0) continue;
+            const float to = best > m[x] + kSlack ? ceilf(best) : m[x];
+            const float alpha = __builtin_amdgcn_exp2f(m[x] - (to == -INFINITY ? 0.f : to));
+            m[x] = to;
+            l[x] *= alpha;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[x][b][i] *= alpha;
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[x][i][h][j] = (__bf16)((float)p[x][i][h][j] * alpha);
+        }
+    };
+
+    f32x16_t s[CB];               // scores of tile t
+    bf16x8_t p[CB][TERMS][2];     // probabilities of tile t - 1
+#pragma unroll
+    for (int x = 0; x < CB; ++x)
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) p[x][i][h] = bf16x8_t{};
+    constexpr int N1 = CB * TERMS * KK, N2 = CB * TERMS * 2 * NB;   // MFMAs of the scores, of the values
+    constexpr int EXPS = 8 * CB, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
+
+    landed(0, min(n_tiles, S - 2) - 1, pg[0]);
+    wait_lgkm<0>();
+    lds_barrier();
+#pragma unroll
+    for (int x = 0; x < CB; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8_t k = key_frag(k_at, kk);
+#pragma unroll
+        for (int x = 0; x < CB; ++x)
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[x][i][kk], s[x], 0, 0, 0);
+    }
+    hide(s, 0, pg[0]);
+    {
+        float top[CB];
+#pragma unroll
+        for (int x = 0; x < CB; ++x) {
+            top[x] = s[x][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top[x] = fmaxf(top[x], s[x][i]);
+        }
+        raise(top, p);
+    }
+    for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
+        landed(t + 1, min(n_tiles, t + S - 2) - (t + 2), pg[1]);
+        wait_lgkm<0>();
+        lds_barrier();   // tile t + 1 has landed, and tile t - 2 has been read by all: its stage takes tile t + S - 2
+        if (t + S - 2 < n_tiles) copy(t + S - 2, pg[S - 2]);
+        const Pages next = pg[1];
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i) pg[i] = pg[i + 1];
+        pg[S - 1] = t + S < n_tiles ? pages_of(t + S) : Pages{{-1, -1}};
+        if (!(active(t - 1) | active(t) | active(t + 1))) continue;   // (p is 0 then, and s -inf)
+
+        const uint32_t kt = k_at + stage(t + 1), vt = v_at + stage(max(t - 1, 0));
+        f32x16_t n[CB];
+        bf16x8_t pn[CB][TERMS][2];
+        float ref[CB], sum[CB];
+#pragma unroll
+        for (int x = 0; x < CB; ++x) {
+            ref[x] = m[x] == -INFINITY ? 0.f : m[x];
+            sum[x] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n[x][i] = 0.f;
+        }
+        auto softmax_piece = [&](int e) {   // scores 2 (e % 8) and the one behind it of block e / 8
+            const int x = e / 8;
+#pragma unroll
+            for (int i = 2 * (e % 8); i < 2 * (e % 8) + 2; ++i) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[x][i], scale, -ref[x]));
+                sum[x] += w;
+                __bf16 b[TERMS];
+                split_terms<TERMS>(w, b);
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) pn[x][j][i / 8][i % 8] = b[j];
+            }
+            asm volatile("" : "+v"(sum[x]));   // (here, and not where the sums are needed)
+        };
+        bf16x8_t kf[2] = {key_frag(kt, 0), key_frag(kt, 1)};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < N1; ++c) {
+            const int kk = c / (CB * TERMS), x = c % (CB * TERMS) / TERMS, i = c % TERMS;
+            n[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk & 1], q[x][i][kk], n[x], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (c % (CB * TERMS) == CB * TERMS - 1 && kk + 2 < KK) kf[kk & 1] = key_frag(kt, kk + 2);
+#pragma unroll
+            for (int e = 0; e < EXPS1; ++e)
+                if (e * N1 / EXPS1 == c) softmax_piece(e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!(active(t + 1) & all_see(a, w_first, w_last, tile_at(t + 1) * KT, KT) & both_known(next))) hide(n, t + 1, next);
+        float top[CB];
+        bf16x8_t vf[2] = {value_frag(vt, 0, 0), value_frag(vt, 0, 1)};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < N2; ++c) {
+            const int f = c / (CB * TERMS), x = c % (CB * TERMS) / TERMS, i = c % TERMS;   // fragment (h, b) = (f / NB, f % NB)
+            o[x][f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f & 1], p[x][i][f / NB], o[x][f % NB], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (c % (CB * TERMS) == CB * TERMS - 1 && f + 2 < 2 * NB) vf[f & 1] = value_frag(vt, (f + 2) / NB, (f + 2) % NB);
+#pragma unroll
+            for (int e = EXPS1; e < EXPS; ++e)
+                if ((e - EXPS1) * N2 / (EXPS - EXPS1) == c) softmax_piece(e);
+#pragma unroll
+            for (int e = 0; e < EXPS; ++e)
+                if (e * N2 / EXPS == c) {
+                    const float pair = fmaxf(n[e / 8][2 * (e % 8)], n[e / 8][2 * (e % 8) + 1]);
+                    top[e / 8] = e % 8 == 0 ? pair : fmaxf(top[e / 8], pair);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int x = 0; x < CB; ++x) {
+            l[x] += sum[x];
+            s[x] = n[x];
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) p[x][i][h] = pn[x][i][h];
+        }
+        raise(top, p);
+    }
+    // whether any wavefront cleared a V
+    __syncthreads();
+    int *const flags = reinterpret_cast<int *>(lds);
+    if (lane == 0) flags[wave] = 0;
+    if (odd) flags[wave] = 1;
+    __syncthreads();
+    if (flags[0] | flags[1] | flags[2] | flags[3]) {   // the cleared elements, key by key
+        const char *const gk = pool + 16 * half, *const gv = pool + hkv * head + 8 * half;
+#pragma unroll 1
+        for (int key = 0; key < n_tiles * KT; ++key) {
+            const int t = key / KT, k0 = tile_at(t) * KT, at = k0 + key % KT, page = at / kPage;
+            if (page > last_page) continue;
+            const int b = ((const_ints)(uintptr_t)seq.table)[page];
+            const Pages two = pages_of(t);
+            if (!known(b) || (all_see(a, first, first + rows - 1, k0, KT) & both_known(two))) continue;
+            const size_t place = (size_t)b * block_bytes + at % kPage * L::ROW;
+#pragma unroll
+            for (int x = 0; x < CB; ++x) {
+                float w = 0.f;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(gk + place + 32 * kk);
+                    float v[8];
+                    load4(a.q, q_at[x] + 16 * kk, TYPE, v);
+                    load4(a.q, q_at[x] + 16 * kk + 4, TYPE, v + 4);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w = fmaf(v[j], (float)k[j], w);
+                    asm volatile("" ::: "memory");   // (registers)
+                }
+                w += lane_xor(w, 32);
+                w = __builtin_amdgcn_exp2f(fmaf(w, a.scale * kLog2e, m[x] == -INFINITY ? 0.f : -m[x]));
+                if (!sees(a, pos[x], at)) continue;
+#pragma unroll
+                for (int c = 0; c < NB; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float v[4];
+                        load4(gv + place, 32 * c + 8 * j, STAGE_BF16, v);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            o[x][c][4 * j + i] = fabsf(v[i]) < INFINITY ? o[x][c][4 * j + i] : fmaf(w, v[i], o[x][c][4 * j + i]);
+                        __builtin_amdgcn_sched_barrier(0);   // (registers)
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < CB; ++x) {
+        const int r = c0 + 32 * x + col, t = r & (bq - 1);
+        const float sum = l[x] + lane_xor(l[x], 32);
+        if (t >= rows) continue;
+        const size_t at = (size_t)(seq.first + t0 + t) * a.out_ld + (size_t)((g << pl.log_g) + (r >> log_bq)) * D + 4 * half;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                store4(a.out, at + 32 * b + 8 * j, TYPE,
+                       quotient(make_float4(o[x][b][4 * j], o[x][b][4 * j + 1], o[x][b][4 * j + 2], o[x][b][4 * j + 3]), sum));
+    }
+}
+
+template <int D, int TERMS, int CB>
+hipError_t launch_tiles(const WindowArgs &a, hipStream_t st) {
+    TilePlan p{};
+    while (a.n_kv_heads << p.log_g < a.n_q_heads) ++p.log_g;
+    // row blocks: no sequence adds more than one that is not full
+    const int bq = 128 * CB >> p.log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
+    const long blocks = ((long)a.rows.rows / bq + seqs) * a.n_kv_heads;
+    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    STG_LAUNCH((window_tiles<D, TERMS, CB>), dim3((unsigned)blocks), dim3(256), 0, st, a, p);
+    return hipGetLastError();
+}
+
+bool by_tiles(const WindowArgs &a) {
+    return a.kv_type == STAGE_BF16 && a.rows.max_rows * (a.n_q_heads / a.n_kv_heads) > 16;
+}
+
 }  // namespace
 
 size_t window_workspace(const WindowArgs &a) {
-    if (a.rows.rows <= 0) return 0;
+    if (a.rows.rows <= 0 || by_tiles(a)) return 0;
     const SplitPlan p = split_plan(a);
     return p.splits == 1 ? 0 : (size_t)a.rows.rows * a.n_q_heads * p.splits * (a.head_dim + 2) * sizeof(float);
 }
@@ -506,6 +926,8 @@ hipError_t launch_window_attention(const WindowArgs &a, hipStream_t st) {
     if (a.rows.rows <= 0) return hipSuccess;
     const bool f32 = a.kv_type == STAGE_F32, exact = a.type == STAGE_F32;
 #define STG_WINDOW_CASE(D)                                                 \
+    if (a.head_dim == D && by_tiles(a))                                    \
+        return exact ? launch_tiles<D, 3, 1>(a, st) : launch_tiles<D, 1, 1>(a, st); \
     if (a.head_dim == D)                                                   \
         return f32 ? launch_split<D, true, 1>(a, st)                       \
                    : exact ? launch_split<D, false, 3>(a, st) : launch_split<D, false, 1>(a, st);
