@@ -587,17 +587,26 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     const size_t head = (size_t)kPage * L::ROW, block_bytes = (size_t)2 * hkv * head;
     const char *const pool = static_cast<const char *>(a.pool) + g * head;
     auto known = [&](int b) { return (unsigned)b < (unsigned)a.rows.n_blocks; };
-    struct Pages { int b[2]; };
-    auto pages_of = [&](int t) {
-        const int p = 2 * tile_at(t);
-        const_ints table = (const_ints)(uintptr_t)seq.table;
-        return Pages{{table[min(p, last_page)], table[min(p + 1, last_page)]}};
-    };
+    // Block ids of the tiles' pages, 64 (32 tiles) in a register of the wavefront, the next 64 under way: loads by
+    // the scalar unit would have every wait for LDS wait for them, too.
+    auto page_at = [&](int t, int h) { return min(2 * tile_at(t) + h, last_page); };
+    auto ids_from = [&](int t) { return seq.table[page_at(t + lane / 2, lane & 1)]; };
+    int ids = 0, more_ids = 0;
+    if (n_tiles > 0) {
+        ids = ids_from(0);
+        more_ids = ids_from(32);
+    }
+    bool strange = __builtin_amdgcn_ballot_w64(!known(ids)) != 0;   // some page so far is not of the pool
     // the wavefront's share of a tile: 8 keys of K and of V, of one page
-    auto copy = [&](int t, const Pages &pg) {
-        const int b = wave < 2 ? pg.b[0] : pg.b[1];
+    auto copy = [&](int t, uint32_t at) {   // (t ascending, each once)
+        if (t > 0 && t % 32 == 0) {
+            ids = more_ids;
+            strange |= __builtin_amdgcn_ballot_w64(!known(ids)) != 0;
+            more_ids = ids_from(t + 32);
+        }
+        const int b = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
         const char *const k = pool + (size_t)(known(b) ? b : 0) * block_bytes + (wave & 1) * 8 * L::ROW;
-        const uint32_t st = ring + t % S * L::BYTES + 8 * wave * L::ROW;
+        const uint32_t st = ring + at + 8 * wave * L::ROW;
         const int r = lane / L::CH, c = lane % L::CH;
 #pragma unroll
         for (int i = 0; i < L::COPIES; ++i) {
@@ -606,12 +615,9 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             dma16(key * L::ROW + 16 * (c ^ L::vx(row)), k + hkv * head, st + L::HALF + 1024 * i);
         }
     };
-    Pages pg[S];   // of tiles t, t + 1, ...
-#pragma unroll
-    for (int i = 0; i < S; ++i) pg[i] = i < n_tiles ? pages_of(i) : Pages{{-1, -1}};
 #pragma unroll
     for (int i = 0; i < S - 2; ++i)
-        if (i < n_tiles) copy(i, pg[i]);
+        if (i < n_tiles) copy(i, i * L::BYTES);
 
     // the wavefront's columns and the rows that they have: positions w_first .. w_last
     const int c0 = 32 * CB * wave, r0 = bq >= 32 * CB ? c0 & (bq - 1) : 0;
@@ -651,23 +657,42 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     const uint32_t k_at = ring + col * L::ROW + 16 * (half ^ L::kx(col));   // chunk 2 kk + half of key col, permuted
     const int vk = 4 * half + (lane & 15) / 4;
     const uint32_t v_at = ring + L::HALF + vk * L::ROW + 8 * (lane & 1) + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ L::vx(vk));
-    auto stage = [&](int t) { return (uint32_t)(t % S * L::BYTES); };
-    auto both_known = [&](const Pages &p) { return known(p.b[0]) & known(p.b[1]); };
-    // (wave-uniform) whether some row of the wavefront sees a key of tile t
-    auto active = [&](int t) {
-        const int k0 = tile_at(t) * KT;
-        return (t >= 0) & (t < n_tiles) & (w_rows > 0) & (k0 <= w_last) & ((k0 < a.sinks) | (k0 + KT - 1 > w_first - a.window));
+    // Turns t as ranges: below `low`, or of [from, from + n).  (Scalar work counts: a turn has few hundred cycles.)
+    struct Turns {
+        int low, from;
+        unsigned n;
+        __device__ __forceinline__ bool has(int t) const { return (t < low) | ((unsigned)(t - from) < n); }
     };
+    // tiles that rows at positions r0 .. r1 (r0 <= r1) all see, and those with a key that some of them sees
+    auto whole = [&](int r0, int r1) {
+        Turns w;
+        w.low = min(sink, max(0, min(min(a.sinks, r0 + 1), a.rows.max_len)) / KT);
+        w.from = sink + max(0, max(0, r1 - a.window + KT) / KT - from);
+        w.n = max(0, sink + max(0, min(r0 + 1, a.rows.max_len)) / KT - from - w.from);
+        return w;
+    };
+    auto touched = [&](int r0, int r1) {   // from a turn before to a turn behind: what a wavefront takes part in
+        Turns w;
+        w.low = min(sink, (max(0, min(min(a.sinks, r1 + 1), a.rows.max_len)) + KT - 1) / KT);
+        if (w.low > 0) ++w.low;
+        w.from = sink + max(0, max(0, r0 - a.window + 1) / KT - from) - 1;
+        const int end = sink + (max(0, min(r1 + 1, a.rows.max_len)) + KT - 1) / KT - from;
+        w.n = end > w.from + 1 ? end + 1 - w.from : 0;
+        return w;
+    };
+    const Turns clear = whole(first, first + rows - 1), my_clear = whole(w_first, max(w_first, w_last));
+    Turns mine = touched(w_first, max(w_first, w_last));
+    if (w_rows <= 0) mine = Turns{0, 0, 0};
     // This wavefront's share of tile t has landed; with the barrier behind it, everybody's.  In a tile that not every
     // row sees, a V that is not finite must not meet the matrix instructions (0 x inf): it becomes 0 here, and is
     // added at the end for the columns that see it.
-    auto landed = [&](int t, int behind, const Pages &p) {   // behind: tiles under way behind it
+    auto landed = [&](int t, uint32_t at, int behind) {   // behind: tiles under way behind it
         if (S > 5 && behind >= 2) wait_vm<(S > 5 ? 2 : 1) * 2 * L::COPIES>();
         else if (S > 4 && behind >= 1) wait_vm<2 * L::COPIES>();
         else wait_vm<0>();
         asm volatile("" ::: "memory");
-        if (t < n_tiles && !(all_see(a, first, first + rows - 1, tile_at(t) * KT, KT) & both_known(p))) {
-            const uint32_t at = ring + stage(t) + L::HALF + 8 * wave * L::ROW + 16 * lane;
+        if ((t < n_tiles) & (!clear.has(t) | strange)) {
+            at += ring + L::HALF + 8 * wave * L::ROW + 16 * lane;
 #pragma unroll
             for (int i = 0; i < L::COPIES; ++i) {
                 u32x4 v = *(lds16)(at + 1024 * i);
@@ -677,14 +702,14 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
         }
     };
-    auto hide = [&](f32x16_t(&s)[CB], int t, const Pages &p) {
+    auto hide = [&](f32x16_t(&s)[CB], int t) {
         const int k0 = tile_at(t) * KT;
-        const bool now = active(t), k1 = known(p.b[0]), k2 = known(p.b[1]);
+        const bool in = t < n_tiles, k1 = in && known(seq.table[page_at(t, 0)]), k2 = in && known(seq.table[page_at(t, 1)]);
 #pragma unroll
         for (int x = 0; x < CB; ++x)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const bool seen = sees(a, pos[x], k0 + 8 * (i / 4) + 4 * half + i % 4) & (i < 8 ? k1 : k2) & now;
+                const bool seen = sees(a, pos[x], k0 + 8 * (i / 4) + 4 * half + i % 4) & (i < 8 ? k1 : k2);
                 s[x][i] = seen ? s[x][i] : -INFINITY;
             }
     };
@@ -731,7 +756,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     constexpr int N1 = CB * TERMS * KK, N2 = CB * TERMS * 2 * NB;   // MFMAs of the scores, of the values
     constexpr int EXPS = 8 * CB, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
 
-    landed(0, min(n_tiles, S - 2) - 1, pg[0]);
+    landed(0, 0, min(n_tiles, S - 2) - 1);
     wait_lgkm<0>();
     lds_barrier();
 #pragma unroll
@@ -746,7 +771,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
 #pragma unroll
             for (int i = 0; i < TERMS; ++i) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[x][i][kk], s[x], 0, 0, 0);
     }
-    hide(s, 0, pg[0]);
+    hide(s, 0);
     {
         float top[CB];
 #pragma unroll
@@ -757,18 +782,19 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         }
         raise(top, p);
     }
+    uint32_t at_new = (S - 2) * L::BYTES, at_next = L::BYTES, at_last = 0;   // stages of tiles t + S - 2, t + 1, t - 1
+    auto step = [&](uint32_t &at) { at = at == (S - 1) * L::BYTES ? 0 : at + L::BYTES; };
     for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
-        landed(t + 1, min(n_tiles, t + S - 2) - (t + 2), pg[1]);
+        landed(t + 1, at_next, min(n_tiles, t + S - 2) - (t + 2));
         wait_lgkm<0>();
         lds_barrier();   // tile t + 1 has landed, and tile t - 2 has been read by all: its stage takes tile t + S - 2
-        if (t + S - 2 < n_tiles) copy(t + S - 2, pg[S - 2]);
-        const Pages next = pg[1];
-#pragma unroll
-        for (int i = 0; i < S - 1; ++i) pg[i] = pg[i + 1];
-        pg[S - 1] = t + S < n_tiles ? pages_of(t + S) : Pages{{-1, -1}};
-        if (!(active(t - 1) | active(t) | active(t + 1))) continue;   // (p is 0 then, and s -inf)
+        if (t + S - 2 < n_tiles) copy(t + S - 2, at_new);
+        const uint32_t kt = k_at + at_next, vt = v_at + at_last;
+        step(at_new);
+        step(at_next);
+        if (t > 0) step(at_last);
+        if (!mine.has(t)) continue;   // (p is 0 then, and s -inf)
 
-        const uint32_t kt = k_at + stage(t + 1), vt = v_at + stage(max(t - 1, 0));
         f32x16_t n[CB];
         bf16x8_t pn[CB][TERMS][2];
         float ref[CB], sum[CB];
@@ -792,29 +818,31 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
             asm volatile("" : "+v"(sum[x]));   // (here, and not where the sums are needed)
         };
-        bf16x8_t kf[2] = {key_frag(kt, 0), key_frag(kt, 1)};
+        bf16x8_t kf[KK], vf[2 * NB];   // (all of K's fragments under way at once, V's while K's are multiplied)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[kk] = key_frag(kt, kk);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < N1; ++c) {
             const int kk = c / (CB * TERMS), x = c % (CB * TERMS) / TERMS, i = c % TERMS;
-            n[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk & 1], q[x][i][kk], n[x], 0, 0, 0);
+            n[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], q[x][i][kk], n[x], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
-            if (c % (CB * TERMS) == CB * TERMS - 1 && kk + 2 < KK) kf[kk & 1] = key_frag(kt, kk + 2);
+#pragma unroll
+            for (int f = 0; f < 2 * NB; ++f)
+                if (f * N1 / (2 * NB) == c) vf[f] = value_frag(vt, f / NB, f % NB);
 #pragma unroll
             for (int e = 0; e < EXPS1; ++e)
                 if (e * N1 / EXPS1 == c) softmax_piece(e);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (!(active(t + 1) & all_see(a, w_first, w_last, tile_at(t + 1) * KT, KT) & both_known(next))) hide(n, t + 1, next);
+        if (!my_clear.has(t + 1) | strange) hide(n, t + 1);
         float top[CB];
-        bf16x8_t vf[2] = {value_frag(vt, 0, 0), value_frag(vt, 0, 1)};
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < N2; ++c) {
             const int f = c / (CB * TERMS), x = c % (CB * TERMS) / TERMS, i = c % TERMS;   // fragment (h, b) = (f / NB, f % NB)
-            o[x][f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f & 1], p[x][i][f / NB], o[x][f % NB], 0, 0, 0);
+            o[x][f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], p[x][i][f / NB], o[x][f % NB], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
-            if (c % (CB * TERMS) == CB * TERMS - 1 && f + 2 < 2 * NB) vf[f & 1] = value_frag(vt, (f + 2) / NB, (f + 2) % NB);
 #pragma unroll
             for (int e = EXPS1; e < EXPS; ++e)
                 if ((e - EXPS1) * N2 / (EXPS - EXPS1) == c) softmax_piece(e);
@@ -850,8 +878,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             const int t = key / KT, k0 = tile_at(t) * KT, at = k0 + key % KT, page = at / kPage;
             if (page > last_page) continue;
             const int b = ((const_ints)(uintptr_t)seq.table)[page];
-            const Pages two = pages_of(t);
-            if (!known(b) || (all_see(a, first, first + rows - 1, k0, KT) & both_known(two))) continue;
+            if (!known(b) || (clear.has(t) && !strange)) continue;
             const size_t place = (size_t)b * block_bytes + at % kPage * L::ROW;
 #pragma unroll
             for (int x = 0; x < CB; ++x) {
