@@ -39,6 +39,22 @@ __device__ __forceinline__ OpRows::Seq uniform(OpRows::Seq s) {
             reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low))};
 }
 
+// Inclusive sums over the lanes (DPP: within rows of 16, then row to row).
+__device__ __forceinline__ int lane_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast 15: rows 0, 2 to 1, 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast 31: row 1 to 2 and 3
+    return v;
+}
+__device__ __forceinline__ const int *lane_pointer(const int *p, int lane) {
+    const uint64_t t = (uint64_t)(uintptr_t)p;
+    const uint32_t low = __builtin_amdgcn_readlane((uint32_t)t, lane), high = __builtin_amdgcn_readlane((uint32_t)(t >> 32), lane);
+    return reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low));
+}
+
 // The pages that rows at positions first .. last see: pages 0 .. sink - 1, then from, from + 1, ...; n in all.
 struct Span {
     int end;          // keys from here on are seen by no row
@@ -516,13 +532,14 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
 // a ring of LDS stages, one barrier per tile.  S^T = K Q^T: lane l holds keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for
 // column l % 32, the k order of the operand P^T of O^T += V^T P^T; 32x32x16 MFMAs, q and p as TERMS bf16 terms.
 //
-// In turn t a wavefront multiplies tile t + 1's K by Q and tile t - 1's V by P while it takes the softmax of
+// In turn t a wavefront multiplies tile t + 1's K by Q and then tile t - 1's V by P while it takes the softmax of
 // tile t: the three are independent, and the vector instructions of the softmax (as long as the MFMAs with one
-// term) are laid between the MFMAs by hand.
+// term) are laid between the MFMAs by hand.  Fragments are in registers half a turn before their MFMAs: V's are
+// read under the scores, K's of the tile behind under the values.
 template <int D, int CB>
 struct TileLds {
     static constexpr int KEYS = 32, ROW = 2 * D, HALF = KEYS * ROW, BYTES = 2 * HALF, CH = ROW / 16;
-    // tile t - 1 is read until the end of turn t: its stage takes tile t + S - 1 in turn t + 1
+    // tile t - 1 is read until the middle of turn t: its stage then takes tile t + S - 1
     static constexpr int STAGES = CB == 1 && D == 128 ? 5 : 6;
     static constexpr int KPC = 1024 / ROW, COPIES = 8 / KPC;   // keys per copy; copies of K (and of V) per wavefront
     __device__ static int kx(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
@@ -554,29 +571,25 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, log_bq = (CB == 1 ? 7 : 8) - pl.log_g, bq = 1 << log_bq;
-    // the sequence and the block of its rows: blocks of all sequences in turn
-    int block = blockIdx.x / hkv, seq_i = 0;
-    for (;; seq_i += 64) {
-        if (seq_i >= a.rows.n_seqs) return;
-        const int i = seq_i + lane;
-        const int own = i < a.rows.n_seqs ? (min(a.rows.seq(i).n, a.rows.max_rows) + bq - 1) >> log_bq : 0;
-        int sum = own;
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) {
-            const int v = __shfl_up(sum, x, 64);
-            if (lane >= x) sum += v;
-        }
+    // the sequence and the block of its rows: blocks of all sequences in turn, 64 sequences at a time
+    int block = blockIdx.x / hkv;
+    OpRows::Seq seq;
+    for (int i0 = 0;; i0 += 64) {
+        if (i0 >= a.rows.n_seqs) return;
+        const int i = min(i0 + lane, a.rows.n_seqs - 1);
+        OpRows::Seq at = a.rows.seq(i);
+        const int own = i0 + lane < a.rows.n_seqs ? (min(at.n, a.rows.max_rows) + bq - 1) >> log_bq : 0, sum = lane_scan(own);
         const int before = __popcll(__builtin_amdgcn_ballot_w64(sum <= block));   // (sums ascend)
         if (before < 64) {
-            const int skipped = __builtin_amdgcn_readlane(sum - own, before), mine = __builtin_amdgcn_readlane(own, before);
-            block = mine - 1 - (block - skipped);      // the last rows, which see the most keys, first
-            seq_i += before;
+            // the last rows, which see the most keys, first
+            block = __builtin_amdgcn_readlane(sum, before) - 1 - block;
+            seq = {__builtin_amdgcn_readlane(at.first, before), __builtin_amdgcn_readlane(at.n, before),
+                   __builtin_amdgcn_readlane(at.pos0, before), lane_pointer(at.table, before)};
             break;
         }
         block -= __builtin_amdgcn_readlane(sum, 63);
     }
-    const OpRows::Seq seq = uniform(a.rows.seq(__builtin_amdgcn_readfirstlane(seq_i)));
-    const int t0 = __builtin_amdgcn_readfirstlane(block) << log_bq, rows = min(bq, min(seq.n, a.rows.max_rows) - t0), first = seq.pos0 + t0;
+    const int t0 = block << log_bq, rows = min(bq, min(seq.n, a.rows.max_rows) - t0), first = seq.pos0 + t0;
     // the tiles that some row sees: 0 .. sink - 1, then from, from + 1, ...
     const int end = min(first + rows, a.rows.max_len), last_page = max(end - 1, 0) / kPage;
     const int sink = (max(0, min(a.sinks, end)) + KT - 1) / KT, from = max(max(0, first - a.window + 1) / KT, sink);
@@ -616,7 +629,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         }
     };
 #pragma unroll
-    for (int i = 0; i < S - 2; ++i)
+    for (int i = 0; i < S - 1; ++i)
         if (i < n_tiles) copy(i, i * L::BYTES);
 
     // the wavefront's columns and the rows that they have: positions w_first .. w_last
@@ -713,7 +726,6 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
                 s[x][i] = seen ? s[x][i] : -INFINITY;
             }
     };
-    auto key_frag = [&](uint32_t k, int kk) { return __builtin_bit_cast(bf16x8_t, *(lds16)(k ^ (32 * kk))); };
     auto value_frag = [&](uint32_t v, int h, int b) {
         const uint32_t at = (v ^ (64 * b)) + 16 * h * L::ROW;
         const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)at);
@@ -756,21 +768,28 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     constexpr int N1 = CB * TERMS * KK, N2 = CB * TERMS * 2 * NB;   // MFMAs of the scores, of the values
     constexpr int EXPS = 8 * CB, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
 
-    landed(0, 0, min(n_tiles, S - 2) - 1);
+    bf16x8_t kf[KK];   // of tile t + 1
+    auto load_keys = [&](uint32_t at) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + at) ^ (32 * kk)));
+    };
+    // tiles 0 and 1 of the S - 1 under way
+    landed(0, 0, min(n_tiles, S - 1) - 2);
+    landed(1, L::BYTES, min(n_tiles, S - 1) - 2);
     wait_lgkm<0>();
     lds_barrier();
+    load_keys(0);
 #pragma unroll
     for (int x = 0; x < CB; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8_t k = key_frag(k_at, kk);
+    for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
         for (int x = 0; x < CB; ++x)
 #pragma unroll
-            for (int i = 0; i < TERMS; ++i) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[x][i][kk], s[x], 0, 0, 0);
-    }
+            for (int i = 0; i < TERMS; ++i) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], q[x][i][kk], s[x], 0, 0, 0);
+    load_keys(L::BYTES);
     hide(s, 0);
     {
         float top[CB];
@@ -782,21 +801,27 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         }
         raise(top, p);
     }
-    uint32_t at_new = (S - 2) * L::BYTES, at_next = L::BYTES, at_last = 0;   // stages of tiles t + S - 2, t + 1, t - 1
+    uint32_t at_new = (S - 1) * L::BYTES, at_keys = 2 * L::BYTES, at_values = 0;   // stages of tiles t + S - 1, t + 2, t - 1
     auto step = [&](uint32_t &at) { at = at == (S - 1) * L::BYTES ? 0 : at + L::BYTES; };
-    for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
-        landed(t + 1, at_next, min(n_tiles, t + S - 2) - (t + 2));
+    // The middle of turn t: tile t + 2 has landed everywhere, and tile t - 1 has been read by all: its stage takes
+    // tile t + S - 1 (tile S - 1 itself goes to the last stage, which is empty)
+    auto middle = [&](int t) {
+        landed(t + 2, at_keys, min(n_tiles, t + S - 1) - (t + 3));
         wait_lgkm<0>();
-        lds_barrier();   // tile t + 1 has landed, and tile t - 2 has been read by all: its stage takes tile t + S - 2
-        if (t + S - 2 < n_tiles) copy(t + S - 2, at_new);
-        const uint32_t kt = k_at + at_next, vt = v_at + at_last;
+        lds_barrier();
+        if (t + S - 1 < n_tiles) copy(t + S - 1, at_new);
+        load_keys(at_keys);
         step(at_new);
-        step(at_next);
-        if (t > 0) step(at_last);
-        if (!mine.has(t)) continue;   // (p is 0 then, and s -inf)
-
+        step(at_keys);
+        if (t > 0) step(at_values);
+    };
+    for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
+        if (!mine.has(t)) {                // (p is 0 then, and s -inf)
+            middle(t);
+            continue;
+        }
         f32x16_t n[CB];
-        bf16x8_t pn[CB][TERMS][2];
+        bf16x8_t pn[CB][TERMS][2], vf[2 * NB];
         float ref[CB], sum[CB];
 #pragma unroll
         for (int x = 0; x < CB; ++x) {
@@ -818,9 +843,6 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
             asm volatile("" : "+v"(sum[x]));   // (here, and not where the sums are needed)
         };
-        bf16x8_t kf[KK], vf[2 * NB];   // (all of K's fragments under way at once, V's while K's are multiplied)
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[kk] = key_frag(kt, kk);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < N1; ++c) {
@@ -829,12 +851,17 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int f = 0; f < 2 * NB; ++f)
-                if (f * N1 / (2 * NB) == c) vf[f] = value_frag(vt, f / NB, f % NB);
+                if (f * N1 / (2 * NB) / 2 == c) vf[f] = value_frag(v_at + at_values, f / NB, f % NB);
 #pragma unroll
             for (int e = 0; e < EXPS1; ++e)
                 if (e * N1 / EXPS1 == c) softmax_piece(e);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (t == 0) {   // no tile before
+#pragma unroll
+            for (int f = 0; f < 2 * NB; ++f) vf[f] = bf16x8_t{};
+        }
+        middle(t);
         if (!my_clear.has(t + 1) | strange) hide(n, t + 1);
         float top[CB];
         __builtin_amdgcn_sched_barrier(0);
@@ -910,18 +937,28 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
         }
     }
+    // Rows are stored 16 bytes a lane, neighbouring lanes side by side, by way of the ring (8 bytes a lane, each row's
+    // over 16 instructions: 30 us more of 320 at 4 x 2048 rows of 64 heads).
+    constexpr int E = TYPE == STAGE_F32 ? 4 : 2, OROW = D * E + 16, OCH = D * E / 16;
+    static_assert(64 + 4 * 32 * OROW <= S * L::BYTES, "the ring holds the output rows");
+    char *const out_lds = lds + 64 + wave * 32 * OROW;   // (behind the flags)
 #pragma unroll
     for (int x = 0; x < CB; ++x) {
-        const int r = c0 + 32 * x + col, t = r & (bq - 1);
         const float sum = l[x] + lane_xor(l[x], 32);
-        if (t >= rows) continue;
-        const size_t at = (size_t)(seq.first + t0 + t) * a.out_ld + (size_t)((g << pl.log_g) + (r >> log_bq)) * D + 4 * half;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                store4(a.out, at + 32 * b + 8 * j, TYPE,
+                store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, TYPE,
                        quotient(make_float4(o[x][b][4 * j], o[x][b][4 * j + 1], o[x][b][4 * j + 2], o[x][b][4 * j + 3]), sum));
+#pragma unroll
+        for (int i = 0; i < 32 * OCH / 64; ++i) {
+            const int e = 64 * i + lane, r = c0 + 32 * x + e / OCH, t = r & (bq - 1);
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(out_lds + e / OCH * OROW + e % OCH * 16);
+            if (t < rows)
+                *reinterpret_cast<u32x4 *>(static_cast<char *>(a.out) + E * ((size_t)(seq.first + t0 + t) * a.out_ld +
+                                           (size_t)((g << pl.log_g) + (r >> log_bq)) * D) + e % OCH * 16) = v;
+        }
     }
 }
 
