@@ -217,7 +217,7 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             p[i] = (sc[i] + s1[i]) * scale;
-            p[i] = !masked | sees(a, pos, k0 + 4 * lq + i) ? p[i] : -INFINITY;
+            p[i] = (!masked | sees(a, pos, k0 + 4 * lq + i)) ? p[i] : -INFINITY;
             top = fmaxf(top, p[i]);
         }
         top = fmaxf(top, lane_xor(top, 16));
@@ -610,23 +610,28 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         more_ids = ids_from(32);
     }
     bool strange = __builtin_amdgcn_ballot_w64(!known(ids)) != 0;   // some page so far is not of the pool
-    // the wavefront's share of a tile: 8 keys of K and of V, of one page
-    auto copy = [&](int t, uint32_t at) {   // (t ascending, each once)
+    // the wavefront's share of a tile: 8 keys of K and of V, of one page, in 2 COPIES instructions
+    const char *copy_from = nullptr;
+    uint32_t copy_to = 0;
+    auto copy_begin = [&](int t, uint32_t at) {   // (t ascending, each once)
         if (t > 0 && t % 32 == 0) {
             ids = more_ids;
             strange |= __builtin_amdgcn_ballot_w64(!known(ids)) != 0;
             more_ids = ids_from(t + 32);
         }
         const int b = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
-        const char *const k = pool + (size_t)(known(b) ? b : 0) * block_bytes + (wave & 1) * 8 * L::ROW;
-        const uint32_t st = ring + at + 8 * wave * L::ROW;
-        const int r = lane / L::CH, c = lane % L::CH;
+        copy_from = pool + (size_t)(known(b) ? b : 0) * block_bytes + (wave & 1) * 8 * L::ROW;
+        copy_to = ring + at + 8 * wave * L::ROW;
+    };
+    auto copy_part = [&](int i) {   // i even: of K, odd: of V
+        const int key = i / 2 * L::KPC + lane / L::CH, row = 8 * wave + key, c = lane % L::CH;
+        if (i & 1) dma16(key * L::ROW + 16 * (c ^ L::vx(row)), copy_from + hkv * head, copy_to + L::HALF + 1024 * (i / 2));
+        else dma16(key * L::ROW + 16 * (c ^ L::kx(row)), copy_from, copy_to + 1024 * (i / 2));
+    };
+    auto copy = [&](int t, uint32_t at) {
+        copy_begin(t, at);
 #pragma unroll
-        for (int i = 0; i < L::COPIES; ++i) {
-            const int key = L::KPC * i + r, row = 8 * wave + key;
-            dma16(key * L::ROW + 16 * (c ^ L::kx(row)), k, st + 1024 * i);
-            dma16(key * L::ROW + 16 * (c ^ L::vx(row)), k + hkv * head, st + L::HALF + 1024 * i);
-        }
+        for (int i = 0; i < 2 * L::COPIES; ++i) copy_part(i);
     };
 #pragma unroll
     for (int i = 0; i < S - 1; ++i)
@@ -715,16 +720,24 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
         }
     };
+    // Bits 0 .. n of a word.
+    auto bits_to = [](int n) { return n < 0 ? 0u : ~0u >> (31 - min(n, 31)); };
     auto hide = [&](f32x16_t(&s)[CB], int t) {
-        const int k0 = tile_at(t) * KT;
-        const bool in = t < n_tiles, k1 = in && known(seq.table[page_at(t, 0)]), k2 = in && known(seq.table[page_at(t, 1)]);
+        const int k0 = tile_at(t) * KT + 4 * half;   // the lane's first key; its others are 8 (i / 4) + i % 4 further
+        uint32_t pages = t < n_tiles ? ~0u : 0u;
+        if (strange && t < n_tiles)
+            pages = (known(seq.table[page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[page_at(t, 1)]) ? 0xFFFF0000u : 0u);
+        pages >>= 4 * half;
 #pragma unroll
-        for (int x = 0; x < CB; ++x)
+        for (int x = 0; x < CB; ++x) {   // (sees(), for 32 keys at once)
+            const uint32_t seen = pages & bits_to(min(pos[x], a.rows.max_len - 1) - k0) &
+                                  (~bits_to(pos[x] - a.window - k0) | bits_to(a.sinks - 1 - k0));
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const bool seen = sees(a, pos[x], k0 + 8 * (i / 4) + 4 * half + i % 4) & (i < 8 ? k1 : k2);
-                s[x][i] = seen ? s[x][i] : -INFINITY;
+                const uint32_t yes = (uint32_t)((int)(seen << (31 - 8 * (i / 4) - i % 4)) >> 31);
+                s[x][i] = __uint_as_float((__float_as_uint(s[x][i]) & yes) | (0xFF800000u & ~yes));
             }
+        }
     };
     auto value_frag = [&](uint32_t v, int h, int b) {
         const uint32_t at = (v ^ (64 * b)) + 16 * h * L::ROW;
@@ -804,13 +817,14 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     uint32_t at_new = (S - 1) * L::BYTES, at_keys = 2 * L::BYTES, at_values = 0;   // stages of tiles t + S - 1, t + 2, t - 1
     auto step = [&](uint32_t &at) { at = at == (S - 1) * L::BYTES ? 0 : at + L::BYTES; };
     // The middle of turn t: tile t + 2 has landed everywhere, and tile t - 1 has been read by all: its stage takes
-    // tile t + S - 1 (tile S - 1 itself goes to the last stage, which is empty)
+    // tile t + S - 1 (tile S - 1 itself goes to the last stage, which is empty).  The copies are then laid between
+    // the values' MFMAs: all wavefronts' at once, behind the barrier, take 580 cycles of a turn of 2200 to issue.
     auto middle = [&](int t) {
         landed(t + 2, at_keys, min(n_tiles, t + S - 1) - (t + 3));
         wait_lgkm<0>();
         lds_barrier();
-        if (t + S - 1 < n_tiles) copy(t + S - 1, at_new);
         load_keys(at_keys);
+        if (t + S - 1 < n_tiles) copy_begin(t + S - 1, at_new);
         step(at_new);
         step(at_keys);
         if (t > 0) step(at_values);
@@ -818,6 +832,10 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
         if (!mine.has(t)) {                // (p is 0 then, and s -inf)
             middle(t);
+            if (t + S - 1 < n_tiles) {
+#pragma unroll
+                for (int i = 0; i < 2 * L::COPIES; ++i) copy_part(i);
+            }
             continue;
         }
         f32x16_t n[CB];
@@ -862,6 +880,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             for (int f = 0; f < 2 * NB; ++f) vf[f] = bf16x8_t{};
         }
         middle(t);
+        const bool more = t + S - 1 < n_tiles;
         if (!my_clear.has(t + 1) | strange) hide(n, t + 1);
         float top[CB];
         __builtin_amdgcn_sched_barrier(0);
@@ -871,13 +890,17 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             o[x][f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], p[x][i][f / NB], o[x][f % NB], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
+            for (int e = 0; e < 2 * L::COPIES; ++e)
+                if (e * N2 / (2 * L::COPIES) == c && more) copy_part(e);
+#pragma unroll
             for (int e = EXPS1; e < EXPS; ++e)
                 if ((e - EXPS1) * N2 / (EXPS - EXPS1) == c) softmax_piece(e);
 #pragma unroll
             for (int e = 0; e < EXPS; ++e)
                 if (e * N2 / EXPS == c) {
-                    const float pair = fmaxf(n[e / 8][2 * (e % 8)], n[e / 8][2 * (e % 8) + 1]);
-                    top[e / 8] = e % 8 == 0 ? pair : fmaxf(top[e / 8], pair);
+                    const float u = n[e / 8][2 * (e % 8)], v = n[e / 8][2 * (e % 8) + 1];
+                    if (e % 8 == 0) top[e / 8] = fmaxf(u, v);
+                    else asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top[e / 8]) : "v"(u), "v"(v));   // (fmaxf quiets each operand first)
                 }
             __builtin_amdgcn_sched_barrier(0);
         }
