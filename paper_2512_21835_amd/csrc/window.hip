@@ -782,9 +782,10 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     constexpr int EXPS = 8 * CB, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
 
     bf16x8_t kf[KK];   // of tile t + 1
+    auto load_key = [&](uint32_t at, int kk) { kf[kk] = __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + at) ^ (32 * kk))); };
     auto load_keys = [&](uint32_t at) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + at) ^ (32 * kk)));
+        for (int kk = 0; kk < KK; ++kk) load_key(at, kk);
     };
     // tiles 0 and 1 of the S - 1 under way
     landed(0, 0, min(n_tiles, S - 1) - 2);
@@ -819,12 +820,13 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     // The middle of turn t: tile t + 2 has landed everywhere, and tile t - 1 has been read by all: its stage takes
     // tile t + S - 1 (tile S - 1 itself goes to the last stage, which is empty).  The copies are then laid between
     // the values' MFMAs: all wavefronts' at once, behind the barrier, take 580 cycles of a turn of 2200 to issue.
+    uint32_t keys_now = 0;
     auto middle = [&](int t) {
         landed(t + 2, at_keys, min(n_tiles, t + S - 1) - (t + 3));
         wait_lgkm<0>();
         lds_barrier();
-        load_keys(at_keys);
         if (t + S - 1 < n_tiles) copy_begin(t + S - 1, at_new);
+        keys_now = at_keys;
         step(at_new);
         step(at_keys);
         if (t > 0) step(at_values);
@@ -832,6 +834,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
         if (!mine.has(t)) {                // (p is 0 then, and s -inf)
             middle(t);
+            load_keys(keys_now);
             if (t + S - 1 < n_tiles) {
 #pragma unroll
                 for (int i = 0; i < 2 * L::COPIES; ++i) copy_part(i);
@@ -892,6 +895,9 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
 #pragma unroll
             for (int e = 0; e < 2 * L::COPIES; ++e)
                 if (e * N2 / (2 * L::COPIES) == c && more) copy_part(e);
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+                if (kk * N2 / KK == c) load_key(keys_now, kk);
 #pragma unroll
             for (int e = EXPS1; e < EXPS; ++e)
                 if ((e - EXPS1) * N2 / (EXPS - EXPS1) == c) softmax_piece(e);
