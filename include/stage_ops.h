@@ -33,7 +33,7 @@ extern "C" {
 #define STAGE_BF16 1
 
 /* Most rows of a call, most sequences, and most block-table entries of a sequence. */
-#define STAGE_OPS_MAX_ROWS 1048576
+#define STAGE_OPS_MAX_ROWS 1048560
 #define STAGE_OPS_MAX_SEQS 65536
 #define STAGE_OPS_MAX_BLOCKS 1048576
 #define STAGE_OPS_MAX_RANK 256

@@ -42,7 +42,7 @@ EXPORTED = (
     "stage_adapter_add",
 )
 STAGE_F32, STAGE_BF16 = 0, 1
-STAGE_OPS_MAX_ROWS = STAGE_OPS_MAX_BLOCKS = 1048576
+STAGE_OPS_MAX_ROWS, STAGE_OPS_MAX_BLOCKS = 1048560, 1048576
 STAGE_OPS_MAX_SEQS = 65536
 STAGE_OPS_MAX_RANK = 256
 STAGE_NOALLOC_SCRATCH_BYTES = 67108864
