@@ -227,63 +227,89 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
         }
     const bool wide = R % 8 == 0;
     const int n_blocks = (a.n + 31) / 32, end = min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
-    for (int nb = blockIdx.x * blocks_per_group + wave / WAYS * BLOCKS; nb < end; nb += 4 / WAYS * BLOCKS) {
-        float y[BLOCKS][8];
-        bool in[BLOCKS];
-        int n[BLOCKS][2];
+    // The blocks, for each the adapters, for each the steps of their ranks: one step's loads of B are under way while
+    // the step before is multiplied (and base's of a block with those of its first step).
+    struct Place { int nb, s, most; unsigned left; int id[IDS], rank[IDS]; };
+    auto take = [&](Place &p) {   // the next adapters of p.left
+        p.s = 0;
+        p.most = 0;
+#pragma unroll
+        for (int u = 0; u < IDS; ++u) {   // (past the last: the first again, of rank 0)
+            const int at = p.left ? __builtin_ctz(p.left) : 0;
+            p.id[u] = p.left ? __builtin_amdgcn_readlane(t.id, at) : u ? p.id[0] : 0;
+            p.rank[u] = p.left ? __builtin_amdgcn_readlane(t.rank, at) : 0;
+            p.most = max(p.most, p.rank[u]);
+            p.left &= p.left - 1;
+        }
+    };
+    auto advance = [&](Place &p) {
+        if (kStep * ++p.s < p.most) return;
+        if (!p.left) {
+            p.nb += 4 / WAYS * BLOCKS;
+            p.left = ids;
+        }
+        take(p);
+    };
+    auto load_b = [&](const Place &p, bf16x8_t (&b)[IDS][BLOCKS][2]) {
+        if (p.nb >= end || p.most == 0) return;
 #pragma unroll
         for (int q = 0; q < BLOCKS; ++q) {
-            const int c = 32 * (nb + q) + 8 * lq, c0 = 32 * (nb + q) + 8 * (l16 / 4) + l16 % 4;
-            in[q] = write && row < a.rows && c < a.n && nb + q < end;
-            if (in[q]) load8(a.base, (size_t)row * a.base_ld + c, TYPE, y[q]);
-            n[q][0] = min(c0, a.n - 1);
-            n[q][1] = min(c0 + 4, a.n - 1);
-        }
-        for (unsigned left = ids; left;) {
-            int id[IDS], rank[IDS], most = 0;
+            const int c0 = 32 * (p.nb + q) + 8 * (l16 / 4) + l16 % 4;
 #pragma unroll
-            for (int u = 0; u < IDS; ++u) {   // (past the last: the first again, of rank 0)
-                const int at = left ? __builtin_ctz(left) : 0;
-                id[u] = left ? __builtin_amdgcn_readlane(t.id, at) : id[0];
-                rank[u] = left ? __builtin_amdgcn_readlane(t.rank, at) : 0;
-                most = max(most, rank[u]);
-                left &= left - 1;
-            }
-            f32x4_t d[IDS][BLOCKS][2];
+            for (int u = 0; u < IDS; ++u)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+                    b[u][q][m] = load_ranks(a.b + ((size_t)p.id[u] * a.n + min(c0 + 4 * m, a.n - 1)) * R, kStep * p.s + 8 * lq, p.rank[u], wide);
+        }
+    };
+    auto mine = [&](int nb) { return write && row < a.rows && 32 * nb + 8 * lq < a.n && nb < end; };
+    auto load_y = [&](int nb, float (&y)[BLOCKS][8]) {
+#pragma unroll
+        for (int q = 0; q < BLOCKS; ++q)
+            if (mine(nb + q)) load8(a.base, (size_t)row * a.base_ld + 32 * (nb + q) + 8 * lq, TYPE, y[q]);
+    };
+    Place at;
+    at.nb = blockIdx.x * blocks_per_group + wave / WAYS * BLOCKS;
+    at.left = ids;
+    take(at);
+    bf16x8_t b[IDS][BLOCKS][2];
+    float y[BLOCKS][8];
+    f32x4_t d[IDS][BLOCKS][2];
+    load_b(at, b);
+    load_y(at.nb, y);
+    while (at.nb < end) {
+        Place to = at;
+        advance(to);
+        bf16x8_t bn[IDS][BLOCKS][2];
+        float yn[BLOCKS][8];
+        load_b(to, bn);
+        if (to.nb != at.nb) load_y(to.nb, yn);
+        if (at.s == 0) {
 #pragma unroll
             for (int u = 0; u < IDS; ++u)
 #pragma unroll
                 for (int q = 0; q < BLOCKS; ++q) d[u][q][0] = d[u][q][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            for (int s = 0; kStep * s < most; ++s) {
-                const int j0 = kStep * s + 8 * lq;
-                bf16x8_t b[IDS][BLOCKS][2];
+        }
+        bf16x8_t x[3];
 #pragma unroll
-                for (int u = 0; u < IDS; ++u)
+        for (int i = 0; i < 3; ++i) x[i] = ts[(min(at.s, rank_steps - 1) * 3 + i) * 64 + lane];
 #pragma unroll
-                    for (int q = 0; q < BLOCKS; ++q)
+        for (int u = 0; u < IDS; ++u) {
+            if (kStep * at.s >= at.rank[u]) continue;
+            const bool cut = kStep * (at.s + 1) > at.rank[u];
 #pragma unroll
-                        for (int m = 0; m < 2; ++m)
-                            b[u][q][m] = load_ranks(a.b + ((size_t)id[u] * a.n + n[q][m]) * R, j0, rank[u], wide);
-                bf16x8_t x[3];
+            for (int q = 0; q < BLOCKS; ++q)
 #pragma unroll
-                for (int i = 0; i < 3; ++i) x[i] = ts[(s * 3 + i) * 64 + lane];
+                for (int m = 0; m < 2; ++m) {
+                    const bf16x8_t f = cut ? cut_ranks(b[u][q][m], kStep * at.s + 8 * lq, at.rank[u]) : b[u][q][m];
 #pragma unroll
-                for (int u = 0; u < IDS; ++u) {
-                    if (kStep * s >= rank[u]) continue;
-                    const bool cut = kStep * (s + 1) > rank[u];
-#pragma unroll
-                    for (int q = 0; q < BLOCKS; ++q)
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const bf16x8_t f = cut ? cut_ranks(b[u][q][m], j0, rank[u]) : b[u][q][m];
-#pragma unroll
-                            for (int i = 0; i < 3; ++i) d[u][q][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, x[i], d[u][q][m], 0, 0, 0);
-                        }
+                    for (int i = 0; i < 3; ++i) d[u][q][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, x[i], d[u][q][m], 0, 0, 0);
                 }
-            }
+        }
+        if (to.s == 0) {   // the adapters' last step
 #pragma unroll
             for (int u = 0; u < IDS; ++u)
-                if (rank[u] > 0 && t.id == id[u]) {
+                if (at.rank[u] > 0 && t.id == at.id[u]) {
 #pragma unroll
                     for (int q = 0; q < BLOCKS; ++q)
 #pragma unroll
@@ -293,9 +319,22 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
                         }
                 }
         }
+        if (to.nb != at.nb) {   // and the block's
 #pragma unroll
-        for (int q = 0; q < BLOCKS; ++q)
-            if (in[q]) store8(a.out, (size_t)row * a.out_ld + 32 * (nb + q) + 8 * lq, TYPE, y[q]);
+            for (int q = 0; q < BLOCKS; ++q)
+                if (mine(at.nb + q)) store8(a.out, (size_t)row * a.out_ld + 32 * (at.nb + q) + 8 * lq, TYPE, y[q]);
+#pragma unroll
+            for (int q = 0; q < BLOCKS; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[q][i] = yn[q][i];
+        }
+        at = to;
+#pragma unroll
+        for (int u = 0; u < IDS; ++u)
+#pragma unroll
+            for (int q = 0; q < BLOCKS; ++q)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) b[u][q][m] = bn[u][q][m];
     }
 }
 
