@@ -137,7 +137,7 @@ typedef struct {
     int32_t max_rank;          /* a multiple of 4, at most STAGE_OPS_MAX_RANK */
     int32_t type;              /* of x, base and out */
     const void *x;             /* [rows, x_ld >= k] */
-    const void *base;          /* [rows, base_ld >= n] */
+    const void *base;          /* [rows, base_ld >= n]; base_ld up to 2^25 */
     void *out;                 /* [rows, out_ld >= n] */
     int64_t x_ld, base_ld, out_ld;
     const void *a;             /* bf16 [n_adapters][max_rank][k] */

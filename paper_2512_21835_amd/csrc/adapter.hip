@@ -5,7 +5,14 @@
 // product of another row's adapter is dropped with its column, so no row's values meet another's.  Bound by bytes: A
 // and B of the adapters present (decode), x, base and out (prompts).  fp32 operands enter as the exact sum of three
 // bf16 terms.
+//
+// Every operand goes through LDS, with neighbouring lanes side by side in memory (weights by copies straight into a
+// ring of each wavefront's own): an MFMA operand read straight from memory has neighbouring lanes in different rows,
+// 55 cache accesses per instruction, which alone took 30 of the up kernel's 53 us at 64 rows of a 70B-shaped projection.
+#include <type_traits>
+
 #include "lanes.h"
+#include "lds_dma.h"
 #include "ops_kernels.h"
 #include "stage_ops.h"
 
@@ -15,6 +22,7 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) u32x4 *lds16;
 
 constexpr int kTile = 16;     // rows of a tile
 constexpr int kStep = 32;     // k (rank) of an MFMA
@@ -81,22 +89,26 @@ struct AdapterPlan {
 };
 
 // t of a tile over a slice of k: a wavefront holds its k of x as operand fragments and takes one item (adapter, 16 of its
-// ranks) after the other, A straight from memory (16 rows x 64 bytes per instruction, all of an item's under way
-// together, the next item's behind them); the four wavefronts' sums meet in LDS.
+// ranks) after the other, its rows of A copied into LDS one item ahead; the four wavefronts' sums meet in LDS.
 constexpr int kWaveK = 256;
 template <int TERMS>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, AdapterPlan pl) {
-    constexpr int TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32, STEPS = kWaveK / kStep;
+    constexpr int TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32, STEPS = kWaveK / kStep, CH = kWaveK / 8;
+    constexpr int STAGE = 16 * kWaveK * 2, COPIES = STAGE / 1024;
+    __shared__ __align__(1024) char ring_lds[4 * 2 * STAGE];
     __shared__ f32x4_t sums[2][4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lq = lane >> 4;
     const int row0 = kTile * blockIdx.x, slice = blockIdx.y;
-    const int k0 = (4 * slice + wave) * pl.wave_k + 8 * lq, k1 = min(a.k, (4 * slice + wave + 1) * pl.wave_k);   // the lane's
+    const int k0 = (4 * slice + wave) * pl.wave_k, k1 = min(a.k, k0 + pl.wave_k);   // the wavefront's (none: k1 <= k0)
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)ring_lds + wave * 2 * STAGE;
+    // x: lane's chunks of eight k, a row's side by side
     float v[STEPS][8];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
+    for (int i = 0; i < STEPS; ++i) {
+        const int e = 64 * i + lane, r = e / CH, k = k0 + e % CH * 8;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[s][j] = 0.f;
-        if (k0 + kStep * s < k1 && row0 + l16 < a.rows) load8(a.x, (size_t)(row0 + l16) * a.x_ld + k0 + kStep * s, TYPE, v[s]);
+        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+        if (k < k1 && row0 + r < a.rows) load8(a.x, (size_t)(row0 + r) * a.x_ld + k, TYPE, v[i]);
     }
     TileIds t;
     t.load(a, row0);
@@ -119,34 +131,68 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, Adapte
     auto skip = [&](int n) {
         for (int i = 0; i < n && left; ++i) next();
     };
-    auto load = [&](const Item &it, u32x4 f[STEPS]) {
-        const uint16_t *const w = a.a + ((size_t)max(it.id, 0) * a.max_rank + min(16 * it.jb + l16, a.max_rank - 1)) * a.k + k0;
+    // chunk c of row r at [r][c ^ r]: every 16 lanes of a fragment's read meet distinct banks
+    auto copy = [&](const Item &it, int stage) {
+        if (it.id < 0 || k0 >= k1) return;
+        const uint16_t *const w = a.a + ((size_t)it.id * a.max_rank + 16 * it.jb) * a.k + k0;
+        const int last = a.max_rank - 1 - 16 * it.jb;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            f[s] = u32x4{0, 0, 0, 0};
-            if (it.id >= 0 && k0 + kStep * s < k1) f[s] = *reinterpret_cast<const u32x4 *>(w + kStep * s);
+        for (int i = 0; i < COPIES; ++i) {
+            const int e = 64 * i + lane, r = e / CH, c = (e % CH) ^ r;
+            // (rows past the last rank: that one; k past the last: the wavefront's first, cleared below)
+            const uint32_t k = k0 + 8 * c < k1 ? 8 * c : 0;
+            dma16(2 * ((uint32_t)min(r, last) * (uint32_t)a.k + k), w, ring + stage * STAGE + 1024 * i);
         }
     };
     skip(blockIdx.z);
     Item it = next();
-    u32x4 f[STEPS];
-    load(it, f);
+    copy(it, 0);
+    // x's fragments, term by term by way of the other stage: chunk c of row r at place 16 (c % 4) + (r ^ c % 16) of step c / 4
     bf16x8_t x[STEPS][TERMS];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) split_terms8<TERMS>(v[s], x[s]);
+    for (int n = 0; n < TERMS; ++n) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int e = 64 * i + lane, r = e / CH, c = e % CH;
+            bf16x8_t b;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                b[j] = (__bf16)v[i][j];
+                v[i][j] -= (float)b[j];
+            }
+            *(lds16)(ring + STAGE + c / 4 * 1024 + 16 * (16 * (c % 4) + (r ^ (c & 15)))) = __builtin_bit_cast(u32x4, b);
+        }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            x[s][n] = __builtin_bit_cast(bf16x8_t, *(lds16)(ring + STAGE + s * 1024 + 16 * (16 * lq + (l16 ^ ((4 * s + lq) & 15)))));
+        asm volatile("" ::: "memory");
+    }
+    const bool tail = k1 - k0 < kWaveK;
     for (int turn = 0; it.id >= 0; ++turn) {
         skip(pl.groups - 1);
         const Item after = next();
-        u32x4 g[STEPS];
-        load(after, g);
+        wait_lgkm<0>();   // the other stage's last readers are done
+        asm volatile("" ::: "memory");
+        copy(after, (turn + 1) & 1);
+        if (after.id >= 0) wait_vm<COPIES>();   // (a wavefront without k waits for nothing)
+        else wait_vm<0>();
+        asm volatile("" ::: "memory");
         f32x4_t d = {0.f, 0.f, 0.f, 0.f};
+        if (k0 < k1) {
+            const uint32_t st = ring + (turn & 1) * STAGE + l16 * (CH * 16);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+            for (int s = 0; s < STEPS; ++s) {
+                u32x4 f = *(lds16)(st + 16 * ((4 * s + lq) ^ l16));
+                if (tail && k0 + kStep * s + 8 * lq >= k1) f = u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < TERMS; ++i)
-                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f[s]), x[s][i], d, 0, 0, 0);
+                for (int i = 0; i < TERMS; ++i)
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f), x[s][i], d, 0, 0, 0);
+            }
+        }
         sums[turn & 1][wave][lane] = d;
-        __syncthreads();
+        wait_lgkm<0>();   // (the copies under way stay so across the barrier)
+        lds_barrier();
         // rank 16 jb + 4 lq + i of row l16
         if (wave == (turn & 3) && t.id == it.id && 16 * it.jb + 4 * lq < a.max_rank) {
             const f32x4_t *const p = &sums[turn & 1][0][lane];
@@ -154,187 +200,250 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, Adapte
                 ((p[0] + p[64]) + p[128]) + p[192];
         }
         it = after;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) f[s] = g[s];
     }
 }
 
-// Eight elements of a row of B from j0 on, of `have` (0: any eight: they are not looked at).
-__device__ __forceinline__ bf16x8_t load_ranks(const uint16_t *w, int j0, int have, bool wide) {
-    u32x4 v;
-    if (wide) {
-        v = *reinterpret_cast<const u32x4 *>(w + (j0 < have ? j0 : 0));
-    } else {   // (rows of a multiple of four)
-        const uint2 x = *reinterpret_cast<const uint2 *>(w + (j0 < have ? j0 : 0)), y = *reinterpret_cast<const uint2 *>(w + (j0 + 4 < have ? j0 + 4 : 0));
-        v = u32x4{x.x, x.y, y.x, y.y};
-    }
-    return __builtin_bit_cast(bf16x8_t, v);
+__device__ __forceinline__ const uint16_t *uniform(const uint16_t *p, int lane) {
+    const uint64_t t = (uint64_t)(uintptr_t)p;
+    const uint32_t low = __builtin_amdgcn_readlane((uint32_t)t, lane), high = __builtin_amdgcn_readlane((uint32_t)(t >> 32), lane);
+    return reinterpret_cast<const uint16_t *>((uintptr_t)((uint64_t)high << 32 | low));
+}
+// Eight elements of a row of B from j0 on, 8 bytes at a time (rows of a multiple of four); past the rank: any.
+__device__ __forceinline__ u32x4 load_ranks(const uint16_t *w, int j0, int rank) {
+    const uint2 x = *reinterpret_cast<const uint2 *>(w + (j0 < rank ? j0 : 0)), y = *reinterpret_cast<const uint2 *>(w + (j0 + 4 < rank ? j0 + 4 : 0));
+    return u32x4{x.x, x.y, y.x, y.y};
 }
 // Elements past the rank become 0.
-__device__ __forceinline__ bf16x8_t cut_ranks(bf16x8_t b, int j0, int rank) {
-    u32x4 v = __builtin_bit_cast(u32x4, b);
+__device__ __forceinline__ u32x4 cut_ranks(u32x4 v, int j0, int rank) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[j] = j0 + 2 * j < rank ? v[j] : 0;
         v[j] = j0 + 2 * j + 1 < rank ? v[j] : v[j] & 0xFFFFu;
     }
-    return __builtin_bit_cast(bf16x8_t, v);
+    return v;
 }
 
-// A workgroup: a tile and 32-column blocks of out.  A wavefront takes BLOCKS of them at a time, with IDS of the tile's
-// adapters at a time, all loads of both under way together.  WAYS wavefronts share the blocks, each with every
-// WAYS-th adapter, whose rows it writes (the first also those without one).  A lane has eight neighbouring columns of a
-// row: MFMA m's row i is column 8 (i / 4) + 4 m + i % 4 of the block.
-template <int TYPE, int WAYS, int IDS, int BLOCKS>
+// At most n memory operations of this wavefront still under way (fewer where n is between two of the counts).
+__device__ __forceinline__ void wait_most(int n) {
+    if (n >= 8) {
+        if (n >= 16) n >= 20 ? wait_vm<20>() : wait_vm<16>();
+        else n >= 12 ? wait_vm<12>() : n >= 10 ? wait_vm<10>() : wait_vm<8>();
+    } else if (n >= 4) {
+        n >= 6 ? wait_vm<6>() : wait_vm<4>();
+    } else {
+        n >= 2 ? wait_vm<2>() : n == 1 ? wait_vm<1>() : wait_vm<0>();
+    }
+}
+
+// A workgroup: a tile and blocks of 64 columns of out, a wavefront each.  A block's items are the tile's adapters, and
+// of each up to 64 ranks at a time; B's of the next two items (and base's of a block with its first) are copied into LDS
+// while one is multiplied; the loop has no load of another kind, whose wait would take in the copies.  WAYS
+// wavefronts share the blocks, each with every WAYS-th adapter, whose rows it writes (the first also those without
+// one).  A lane has 16 neighbouring columns of a row: MFMA m's row i is column 16 (i / 4) + 4 m + i % 4 of the block.
+//
+// A turn is as long as the latency of its own instructions, of one or two wavefronts per SIMD, so it has few: the items,
+// the same for every block, are listed once, an item per lane; t's fragments stay in registers.
+constexpr int kCols = 64, kRanks = 64;
+template <int TYPE>
+struct UpLds {   // a wavefront's: S stages of B (by the adapters' rank), S of base
+    static constexpr int S = 3, E = TYPE == STAGE_F32 ? 4 : 2, Y_STAGE = kTile * kCols * E, YCOPIES = Y_STAGE / 1024;
+    static constexpr int b_stage(int max_rank) { return kCols * 2 * (max_rank > 32 ? 64 : max_rank > 16 ? 32 : 16); }
+    static constexpr int bytes(int max_rank) { return S * (b_stage(max_rank) + Y_STAGE); }
+};
+template <int TYPE, int WAYS, int T_STEPS>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterPlan pl, int blocks_per_group) {
-    extern __shared__ __align__(16) char lds[];
-    bf16x8_t *const ts = reinterpret_cast<bf16x8_t *>(lds);   // t as operand fragments, [rank step][term][lane]
+    using L = UpLds<TYPE>;
+    constexpr int S = L::S, E = L::E, YCOPIES = L::YCOPIES, YCH = kCols * E / 16;
+    extern __shared__ __align__(1024) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int row0 = kTile * blockIdx.y, R = a.max_rank, rank_steps = (R + kStep - 1) / kStep;
+    const int row0 = kTile * blockIdx.y, R = a.max_rank, b_stage = L::b_stage(R);
     const int row = row0 + l16;
     TileIds t;
     t.load(a, row0);
-    const float scale = a.scales && t.id >= 0 ? a.scales[t.id] : 1.f;
-    for (int s = wave; s < rank_steps; s += 4) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const int j0 = kStep * s + 8 * lq;
-#pragma unroll
-        for (int h = 0; h < 8; h += 4) {
-            if (j0 + h >= t.rank) continue;
-            const float *p = a.part + (size_t)row * R + j0 + h;
-            f32x4_t sum = *reinterpret_cast<const f32x4_t *>(p);
-#pragma unroll 8
-            for (int sl = 1; sl < pl.slices; ++sl) sum += *reinterpret_cast<const f32x4_t *>(p + (size_t)sl * a.rows * R);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[h + j] = j0 + h + j < t.rank ? sum[j] * scale : 0.f;
-        }
-        bf16x8_t b[3];
-        split_terms8<3>(v, b);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) ts[(s * 3 + i) * 64 + lane] = b[i];
-    }
-    __syncthreads();
-    // this wavefront's adapters, and whether this lane's row is its to write
+    // this wavefront's items, an item per lane: B's first place for it, how many of the adapter's ranks are left, and
+    // the adapter; and whether the lane's row is its to write
     const int way = wave % WAYS;
-    unsigned ids = 0;
-    int seen = 0;
+    const uint16_t *item_b = nullptr;
+    int item_ranks = 0, item_id = -1, n_items = 0, seen = 0;
     bool write = t.id < 0 && way == 0;
     for (unsigned left = t.first; left; left &= left - 1, ++seen)
         if (seen % WAYS == way) {
-            const int at = __builtin_ctz(left);
-            ids |= 1u << at;
-            write |= (t.id >= 0) & (__builtin_amdgcn_readlane(t.id, at) == t.id);
+            const int at = __builtin_ctz(left), id = __builtin_amdgcn_readlane(t.id, at), rank = __builtin_amdgcn_readlane(t.rank, at);
+            const int mine = lane - n_items;
+            if (mine >= 0 && kRanks * mine < rank) {
+                item_b = a.b + (size_t)id * a.n * R + kRanks * mine;
+                item_ranks = rank - kRanks * mine;
+                item_id = id;
+            }
+            n_items += (rank + kRanks - 1) / kRanks;
+            write |= t.id == id;
         }
-    const bool wide = R % 8 == 0;
-    const int n_blocks = (a.n + 31) / 32, end = min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
-    // The blocks, for each the adapters, for each the steps of their ranks: one step's loads of B are under way while
-    // the step before is multiplied (and base's of a block with those of its first step).
-    struct Place { int nb, s, most; unsigned left; int id[IDS], rank[IDS]; };
-    auto take = [&](Place &p) {   // the next adapters of p.left
-        p.s = 0;
-        p.most = 0;
-#pragma unroll
-        for (int u = 0; u < IDS; ++u) {   // (past the last: the first again, of rank 0)
-            const int at = p.left ? __builtin_ctz(p.left) : 0;
-            p.id[u] = p.left ? __builtin_amdgcn_readlane(t.id, at) : u ? p.id[0] : 0;
-            p.rank[u] = p.left ? __builtin_amdgcn_readlane(t.rank, at) : 0;
-            p.most = max(p.most, p.rank[u]);
-            p.left &= p.left - 1;
-        }
-    };
+    write &= row < a.rows;
+    if (n_items == 0) n_items = 1;   // (of no rank: base to out)
+    const bool any = __builtin_amdgcn_ballot_w64(write) != 0, wide = R % 8 == 0;
+    const int n_blocks = (a.n + kCols - 1) / kCols, end = min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * L::bytes(R);
+    const uint32_t y_ring = ring + S * b_stage;
+
+    struct Place { int nb, slot, item, ranks, copies; };   // block and its place in y_ring, item, its ranks, its copies
+    auto fill = [&](Place &p) { p.ranks = p.nb < end ? __builtin_amdgcn_readlane(item_ranks, p.item) : 0; };
     auto advance = [&](Place &p) {
-        if (kStep * ++p.s < p.most) return;
-        if (!p.left) {
-            p.nb += 4 / WAYS * BLOCKS;
-            p.left = ids;
+        if (++p.item == n_items) {
+            p.item = 0;
+            p.nb += 4 / WAYS;
+            p.slot = p.slot == S - 1 ? 0 : p.slot + 1;
         }
-        take(p);
+        fill(p);
     };
-    auto load_b = [&](const Place &p, bf16x8_t (&b)[IDS][BLOCKS][2]) {
-        if (p.nb >= end || p.most == 0) return;
+    // log2 of the 16-byte chunks that the item's rows have in LDS: 2, 4 or 8
+    auto log_chunks = [](int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 3; };
+    // chunk c of row r lies at c ^ place(r): every 16 lanes of a fragment's read meet distinct banks (two chunks: pairs)
+    auto place = [](int r, int lc) { return ((r & 3) | (r >> 4 & 3) << 2) >> (4 - lc); };
+    auto y_place = [](int r) { return YCH == 16 ? r : r >> 1; };   // (likewise, of 16 rows of base)
+    auto copy = [&](Place &p, uint32_t at) {
+        p.copies = 0;
+        if (p.nb >= end) return;
+        if (p.item == 0) {   // base: rows past the last: that one; columns past the last: the first
+            p.copies = YCOPIES;
+            const char *const from = static_cast<const char *>(a.base) + E * ((size_t)row0 * a.base_ld + (size_t)kCols * p.nb);
 #pragma unroll
-        for (int q = 0; q < BLOCKS; ++q) {
-            const int c0 = 32 * (p.nb + q) + 8 * (l16 / 4) + l16 % 4;
+            for (int i = 0; i < YCOPIES; ++i) {
+                const int e = 64 * i + lane, r = e / YCH, c = ((e % YCH) ^ y_place(r)) * (16 / E);
+                dma16(E * ((uint32_t)min(r, a.rows - 1 - row0) * (uint32_t)a.base_ld + (kCols * p.nb + c < a.n ? c : 0)), from,
+                      y_ring + (p.slot * YCOPIES + i) * 1024);
+            }
+        }
+        if (p.ranks == 0 || !wide) return;
+        const int lc = log_chunks(p.ranks), n = 1 << lc;
+        p.copies += n;
+        const uint16_t *const w = uniform(item_b, p.item) + (size_t)kCols * p.nb * R;
+        const int last = a.n - 1 - kCols * p.nb;
 #pragma unroll
-            for (int u = 0; u < IDS; ++u)
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-                    b[u][q][m] = load_ranks(a.b + ((size_t)p.id[u] * a.n + min(c0 + 4 * m, a.n - 1)) * R, kStep * p.s + 8 * lq, p.rank[u], wide);
+        for (int i = 0; i < 8; ++i) {
+            if (i >= n) break;
+            const int e = 64 * i + lane, r = e >> lc, c = (e & ((1 << lc) - 1)) ^ place(r, lc);
+            // (rows past the last column: that one; chunks past the rank: the first, cut below)
+            dma16(2 * ((uint32_t)min(r, last) * R + (8 * c < p.ranks ? 8 * c : 0)), w, at + 1024 * i);
         }
     };
-    auto mine = [&](int nb) { return write && row < a.rows && 32 * nb + 8 * lq < a.n && nb < end; };
-    auto load_y = [&](int nb, float (&y)[BLOCKS][8]) {
+    Place p0{(int)blockIdx.x * blocks_per_group + wave / WAYS, 0, 0, 0, 0};
+    fill(p0);
+    copy(p0, ring);
+    Place p1 = p0;
+    advance(p1);
+    copy(p1, ring + b_stage);
+
+    // t as operand fragments: the slices added
+    const float scale = a.scales && t.id >= 0 ? a.scales[t.id] : 1.f;
+    bf16x8_t x[T_STEPS][3];
 #pragma unroll
-        for (int q = 0; q < BLOCKS; ++q)
-            if (mine(nb + q)) load8(a.base, (size_t)row * a.base_ld + 32 * (nb + q) + 8 * lq, TYPE, y[q]);
-    };
-    Place at;
-    at.nb = blockIdx.x * blocks_per_group + wave / WAYS * BLOCKS;
-    at.left = ids;
-    take(at);
-    bf16x8_t b[IDS][BLOCKS][2];
-    float y[BLOCKS][8];
-    f32x4_t d[IDS][BLOCKS][2];
-    load_b(at, b);
-    load_y(at.nb, y);
-    while (at.nb < end) {
-        Place to = at;
-        advance(to);
-        bf16x8_t bn[IDS][BLOCKS][2];
-        float yn[BLOCKS][8];
-        load_b(to, bn);
-        if (to.nb != at.nb) load_y(to.nb, yn);
-        if (at.s == 0) {
+    for (int s = 0; s < T_STEPS; ++s) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const int j0 = kStep * s + 8 * lq;
+        const float *const p = a.part + (size_t)min(row, a.rows - 1) * R + min(j0, R - 4);
+        const int more = j0 + 4 < R ? 4 : 0;   // (ranks that are none are read all the same, and dropped)
+        for (int s0 = 0; kStep * s < R && s0 < pl.slices; s0 += 8) {
+            f32x4_t u[8], w[8];
 #pragma unroll
-            for (int u = 0; u < IDS; ++u)
+            for (int i = 0; i < 8; ++i) {
+                const size_t at = (size_t)min(s0 + i, pl.slices - 1) * a.rows * R;
+                u[i] = *reinterpret_cast<const f32x4_t *>(p + at);
+                w[i] = *reinterpret_cast<const f32x4_t *>(p + at + more);
+            }
 #pragma unroll
-                for (int q = 0; q < BLOCKS; ++q) d[u][q][0] = d[u][q][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
-        bf16x8_t x[3];
+            for (int i = 0; i < 8; ++i)
+                if (s0 + i < pl.slices) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i) x[i] = ts[(min(at.s, rank_steps - 1) * 3 + i) * 64 + lane];
-#pragma unroll
-        for (int u = 0; u < IDS; ++u) {
-            if (kStep * at.s >= at.rank[u]) continue;
-            const bool cut = kStep * (at.s + 1) > at.rank[u];
-#pragma unroll
-            for (int q = 0; q < BLOCKS; ++q)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const bf16x8_t f = cut ? cut_ranks(b[u][q][m], kStep * at.s + 8 * lq, at.rank[u]) : b[u][q][m];
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) d[u][q][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, x[i], d[u][q][m], 0, 0, 0);
+                    for (int j = 0; j < 4; ++j) {
+                        v[j] += u[i][j];
+                        v[4 + j] += w[i][j];
+                    }
                 }
         }
-        if (to.s == 0) {   // the adapters' last step
 #pragma unroll
-            for (int u = 0; u < IDS; ++u)
-                if (at.rank[u] > 0 && t.id == at.id[u]) {
+        for (int j = 0; j < 8; ++j) v[j] = j0 + j < t.rank ? v[j] * scale : 0.f;
+        split_terms8<3>(v, x[s]);
+    }
+    f32x4_t d[4], sum[4];   // of the adapter; of the row's adapter
+    int stores1 = 0, stores2 = 0, first_step = 0;   // stores of the turn before, and of the one before that
+    uint32_t at = ring;
+    while (p0.nb < end) {
+        Place p2 = p1;
+        advance(p2);
+        wait_lgkm<0>();   // the stage's last readers are done
+        asm volatile("" ::: "memory");
+        copy(p2, at == ring ? ring + 2 * b_stage : at - b_stage);
+        wait_most(p1.copies + p2.copies + stores1 + stores2);
+        asm volatile("" ::: "memory");
+        stores2 = stores1;
+        stores1 = 0;
+        const int id = __builtin_amdgcn_readlane(item_id, p0.item), lc = log_chunks(p0.ranks);
+        u32x4 f[2][4];
 #pragma unroll
-                    for (int q = 0; q < BLOCKS; ++q)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            y[q][i] += d[u][q][0][i];
-                            y[q][4 + i] += d[u][q][1][i];
+            for (int m = 0; m < 4; ++m) {
+                const int r = 16 * (l16 >> 2) + 4 * m + (l16 & 3), c = 4 * e + lq;
+                f[e][m] = u32x4{0, 0, 0, 0};
+                if (kStep * e >= p0.ranks) continue;
+                if (wide) f[e][m] = *(lds16)(at + 16 * ((r << lc) + ((c & ((1 << lc) - 1)) ^ place(r, lc))));
+                else f[e][m] = load_ranks(uniform(item_b, p0.item) + (size_t)min(kCols * p0.nb + r, a.n - 1) * R, 8 * c, p0.ranks);
+                if (kStep * (e + 1) > p0.ranks) f[e][m] = cut_ranks(f[e][m], kStep * e + 8 * lq, p0.ranks);
+            }
+        if (first_step == 0) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) d[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int s = 0; s < T_STEPS; s += 2) {
+            if (s != first_step) continue;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (kStep * e >= p0.ranks || s + e >= T_STEPS) break;
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        d[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f[e][m]), x[s + e < T_STEPS ? s + e : 0][i], d[m], 0, 0, 0);
+            }
+        }
+        const bool last = p0.ranks <= kRanks;   // of the adapter
+        first_step = last ? 0 : first_step + 2;
+        if (last && t.id == id) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) sum[m] = d[m];
+        }
+        if (p1.nb != p0.nb) {   // the block's last
+            if (any) stores1 = E;
+            const int c0 = kCols * p0.nb + 16 * lq;
+            if (write && c0 < a.n) {
+                const uint32_t from = y_ring + p0.slot * L::Y_STAGE + l16 * (16 * YCH);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {   // eight columns
+                    float y[8];
+                    if constexpr (TYPE == STAGE_F32) {
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            const f32x4_t u = __builtin_bit_cast(f32x4_t, *(lds16)(from + 16 * ((4 * lq + 2 * h + g) ^ y_place(l16))));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[4 * g + i] = u[i];
                         }
+                    } else {
+                        const bf16x8_t u = __builtin_bit_cast(bf16x8_t, *(lds16)(from + 16 * ((2 * lq + h) ^ y_place(l16))));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = (float)u[i];
+                    }
+                    if (t.id >= 0) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] += sum[2 * h + i / 4][i % 4];
+                    }
+                    if (c0 + 8 * h < a.n) store8(a.out, (size_t)row * a.out_ld + c0 + 8 * h, TYPE, y);
                 }
+            }
         }
-        if (to.nb != at.nb) {   // and the block's
-#pragma unroll
-            for (int q = 0; q < BLOCKS; ++q)
-                if (mine(at.nb + q)) store8(a.out, (size_t)row * a.out_ld + 32 * (at.nb + q) + 8 * lq, TYPE, y[q]);
-#pragma unroll
-            for (int q = 0; q < BLOCKS; ++q)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[q][i] = yn[q][i];
-        }
-        at = to;
-#pragma unroll
-        for (int u = 0; u < IDS; ++u)
-#pragma unroll
-            for (int q = 0; q < BLOCKS; ++q)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) b[u][q][m] = bn[u][q][m];
+        p0 = p1;
+        p1 = p2;
+        at = at == ring + 2 * b_stage ? ring : at + b_stage;
     }
 }
 
@@ -352,18 +461,29 @@ AdapterPlan adapter_plan(const AdapterArgs &a) {
 }
 
 template <int TYPE>
-void launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles, hipStream_t st) {
-    const int blocks = (a.n + 31) / 32;
-    const long want = 4L * device_compute_units();   // workgroups
-    // few tiles: their wavefronts share the adapters, four at a time; many: four blocks at a time
+hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles, hipStream_t st) {
+    const int blocks = (a.n + kCols - 1) / kCols, lds = 4 * UpLds<TYPE>::bytes(a.max_rank);
+    const long want = (long)(160 * 1024 / lds) * device_compute_units();   // workgroups: as many as run at once
+    // few tiles: the wavefronts share a block's adapters; many: a block each
     const bool shared = p.groups > 1 && a.n_adapters >= 4;
-    const int least = shared ? 1 : 16;
+    const int least = shared ? 1 : 4;
     long per = ((long)blocks * tiles + want - 1) / want;
     per = (per + least - 1) / least * least;
-    const size_t t_lds = (size_t)(a.max_rank + kStep - 1) / kStep * 3 * 1024;
     const dim3 grid((unsigned)((blocks + per - 1) / per), tiles);
-    if (shared) STG_LAUNCH((adapter_up_kernel<TYPE, 4, 4, 1>), grid, dim3(256), t_lds, st, a, p, (int)per);
-    else STG_LAUNCH((adapter_up_kernel<TYPE, 1, 1, 4>), grid, dim3(256), t_lds, st, a, p, (int)per);
+    auto launch = [&](auto ways, auto steps) -> hipError_t {
+        auto *const kernel = adapter_up_kernel<TYPE, decltype(ways)::value, decltype(steps)::value>;
+        // (more LDS than a launch may take unasked)
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        STG_LAUNCH(kernel, grid, dim3(256), lds, st, a, p, (int)per);
+        return hipGetLastError();
+    };
+    using One = std::integral_constant<int, 1>;
+    using Four = std::integral_constant<int, 4>;
+    using Few = std::integral_constant<int, kRanks / kStep>;
+    using Most = std::integral_constant<int, STAGE_OPS_MAX_RANK / kStep>;
+    if (a.max_rank <= kRanks) return shared ? launch(Four{}, Few{}) : launch(One{}, Few{});
+    return shared ? launch(Four{}, Most{}) : launch(One{}, Most{});
 }
 
 }  // namespace
@@ -380,12 +500,11 @@ hipError_t launch_adapter_add(const AdapterArgs &a, hipStream_t st) {
     const dim3 down(tiles, p.slices, p.groups);
     if (a.type == STAGE_F32) {
         STG_LAUNCH(adapter_down_kernel<3>, down, dim3(256), 0, st, a, p);
-        launch_up<STAGE_F32>(a, p, tiles, st);
+        return launch_up<STAGE_F32>(a, p, tiles, st);
     } else {
         STG_LAUNCH(adapter_down_kernel<1>, down, dim3(256), 0, st, a, p);
-        launch_up<STAGE_BF16>(a, p, tiles, st);
+        return launch_up<STAGE_BF16>(a, p, tiles, st);
     }
-    return hipGetLastError();
 }
 
 }  // namespace stg

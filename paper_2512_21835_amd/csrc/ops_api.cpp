@@ -217,7 +217,7 @@ int stage_adapter_add(const stage_adapter_args *p, void *workspace, int64_t work
     if (!adapter_sizes(a) || !rows_ok(a.x, a.x_ld, a.k, a.type) || !rows_ok(a.base, a.base_ld, a.n, a.type) ||
         !rows_ok(a.out, a.out_ld, a.n, a.type) || !a.a || !a.b || !on16(a.a) || !on16(a.b) || !a.ids)
         return STAGE_EINVAL;
-    if (a.out == a.base && a.out_ld != a.base_ld) return STAGE_EINVAL;
+    if ((a.out == a.base && a.out_ld != a.base_ld) || a.base_ld > (int64_t(1) << 25)) return STAGE_EINVAL;   // (16 rows within 32 bits)
     if (!device_ok(a.device)) return STAGE_EINVAL;
     DeviceGuard dg(a.device);
     const AdapterArgs w = adapter_args(a, workspace);

@@ -8,8 +8,9 @@ from torch's allocator, on that stream.
 from __future__ import annotations
 
 import ctypes
+import struct
 from ctypes import c_float, c_int32, c_int64, c_void_p
-from typing import Optional, Sequence
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -50,10 +51,19 @@ class StageAdapterArgs(ctypes.Structure):
                 ("ids", c_void_p), ("ranks", c_void_p), ("scales", c_void_p)]
 
 
+# A call's argument struct as one pack() (a tenth of the time of filling a ctypes structure field by field; the
+# classes above are the same layouts for programs that call the library themselves).  "40s" is a StageBatch.
+_BATCH = struct.Struct("@iiiiPPP")
+_APPEND = struct.Struct("@i4x40sPiiii ii PP qq ii PP fi PPP iiii")
+_WINDOW = struct.Struct("@i4x40sPiiii ii iif4x PP qq i4x")
+_ADAPTER = struct.Struct("@iiiiiii4x PPP qqq PPP PP")
+
+
 def _device(t: torch.Tensor) -> int:
-    if not t.is_cuda:
+    device = t.get_device()
+    if device < 0:
         raise ValueError("tensors must be on a GPU")
-    return t.device.index
+    return device
 
 
 def _type(t: torch.Tensor) -> int:
@@ -63,65 +73,76 @@ def _type(t: torch.Tensor) -> int:
     return kind
 
 
-def _plain(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: Sequence[int], device: int) -> Optional[int]:
-    """Address of a contiguous tensor of this type, shape (None: any) and device; None for none."""
+def _plain(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: Tuple[int, ...], device: int) -> int:
+    """Address of a contiguous tensor of this type, shape and device; 0 for none."""
     if t is None:
-        return None
-    if t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or _device(t) != device:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {len(shape)} dimensions on the call's device")
-    for have, want in zip(t.shape, shape):
-        if want is not None and have != want:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is needed")
+        return 0
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {shape} on the call's device, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _row_stride(t: torch.Tensor, name: str, device: int) -> int:
     """Elements from row to row of [rows, width] or [rows, heads, head_dim], whose rows are each contiguous."""
-    shape, stride = t.shape, t.stride()
-    if _device(t) != device:
+    shape = t.shape
+    if t.get_device() != device:
         raise ValueError(f"{name} is on another device")
-    width = 1
-    for n, s in zip(reversed(shape[1:]), reversed(stride[1:])):
-        if n != 1 and s != width:
-            raise ValueError(f"the rows of {name} must be contiguous")
-        width *= n
+    width = shape[-1] if len(shape) == 2 else shape[1] * shape[2]
+    if t.is_contiguous():
+        return width
+    stride = t.stride()
+    if (stride[-1] != 1 and shape[-1] != 1) or (len(shape) == 3 and stride[1] != shape[2] and shape[1] != 1):
+        raise ValueError(f"the rows of {name} must be contiguous")
     return stride[0] if shape[0] > 1 else width
 
 
-def _cache(pool: torch.Tensor, device: int) -> StageCache:
-    if pool.dim() != 5 or pool.shape[1] != 2 or pool.shape[3] != 16 or not pool.is_contiguous() or _device(pool) != device:
+def _cache(pool: torch.Tensor, device: int) -> Tuple[int, int, int, int, int]:
+    shape = pool.shape
+    if len(shape) != 5 or shape[1] != 2 or shape[3] != 16 or not pool.is_contiguous() or pool.get_device() != device:
         raise ValueError("pool must be a contiguous tensor [n_blocks, 2, n_kv_heads, 16, head_dim] on the call's device")
-    return StageCache(pool.data_ptr(), pool.shape[0], pool.shape[2], pool.shape[4], _type(pool))
+    return pool.data_ptr(), shape[0], shape[2], shape[4], _type(pool)
 
 
-def _batch(batch: StageBatch, device: int) -> StageBatch:
+def _batch(batch: StageBatch, device: int) -> bytes:
     if batch.device != device:
         raise ValueError("the batch is on another device")
-    return batch
+    return batch.raw
 
 
-def _workspace(size, args, device: int, given: Optional[torch.Tensor], stream):
-    """The workspace tensor of a call (None: it takes none)."""
+def _workspace(size, args: bytes, device: int, given: Optional[torch.Tensor], stream):
+    """Address and bytes of the workspace of a call, and what keeps it."""
     if given is not None:
-        if not given.is_contiguous() or _device(given) != device:
+        if not given.is_contiguous() or given.get_device() != device:
             raise ValueError("the workspace must be a contiguous tensor on the call's device")
-        return given
+        return given.data_ptr(), given.nbytes, given
     need = c_int64()
-    _check(size(ctypes.byref(args), ctypes.byref(need)))
+    rc = size(args, ctypes.byref(need))
+    if rc:
+        _check(rc)
     if need.value == 0:
-        return None
+        return None, 0, None
     if stream is None:
-        return torch.empty(need.value, dtype=torch.uint8, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(need.value, dtype=torch.uint8, device=device)
+        given = torch.empty(need.value, dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(stream):
+            given = torch.empty(need.value, dtype=torch.uint8, device=device)
+    return given.data_ptr(), need.value, given
 
 
 def _handle(stream, device: int) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device.index != device:
+        return _current_stream(device)
+    if stream.device.index != device:
         raise ValueError("the stream is on another device")
     return stream.cuda_stream
+
+
+def _current_stream(device: int) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):   # (the same handle, without a stream object)
+    _current_stream = torch._C._cuda_getCurrentRawStream  # noqa: F811
 
 
 def stage_batch(row_start: torch.Tensor, length: torch.Tensor, block_table: torch.Tensor, max_rows: int,
@@ -129,10 +150,12 @@ def stage_batch(row_start: torch.Tensor, length: torch.Tensor, block_table: torc
     """The sequences of a call: int32 row_start [n + 1], length [n] and block_table [n, max_blocks]; no sequence
     has more than max_rows rows or holds more than max_len tokens."""
     device, n = _device(row_start), length.shape[0]
-    b = StageBatch(n, max_rows, max_len, block_table.shape[-1], _plain(row_start, "row_start", torch.int32, (n + 1,), device),
-                   _plain(length, "length", torch.int32, (n,), device),
-                   _plain(block_table, "block_table", torch.int32, (n, None), device))
-    b.device, b.tensors = device, (row_start, length, block_table)
+    blocks = block_table.shape[-1]
+    raw = _BATCH.pack(n, max_rows, max_len, blocks, _plain(row_start, "row_start", torch.int32, (n + 1,), device),
+                      _plain(length, "length", torch.int32, (n,), device),
+                      _plain(block_table, "block_table", torch.int32, (n, blocks), device))
+    b = StageBatch.from_buffer_copy(raw)
+    b.raw, b.device, b.tensors = raw, device, (row_start, length, block_table)
     return b
 
 
@@ -145,43 +168,48 @@ def stage_norm_rope_append(qkv: torch.Tensor, q_out: torch.Tensor, pool: torch.T
     d].  positions int32 [rows], or [3, rows] with the pairs per axis in ``sections``."""
     device = _device(qkv)
     cache = _cache(pool, device)
-    d, hkv = cache.head_dim, cache.n_kv_heads
-    if qkv.dim() != 3 or q_out.dim() != 3 or qkv.shape[2] != d or q_out.shape[2] != d or q_out.shape[0] != qkv.shape[0] or \
-            qkv.shape[1] != q_out.shape[1] + 2 * hkv:
+    d, hkv = cache[3], cache[2]
+    if qkv.dim() != 3 or q_out.dim() != 3:
+        raise ValueError("qkv and q_out have three dimensions: rows, heads, head_dim")
+    rows, hq, angles = qkv.shape[0], q_out.shape[1], cos.shape[0]
+    if qkv.shape != (rows, hq + 2 * hkv, d) or q_out.shape != (rows, hq, d):
         raise ValueError(f"qkv {tuple(qkv.shape)}, q_out {tuple(q_out.shape)} and pool {tuple(pool.shape)} do not fit")
-    rows, axes = qkv.shape[0], 1 if positions is None or positions.dim() == 1 else 3
+    axes = 1 if positions is None or positions.dim() == 1 else 3
     if positions is not None and (axes == 3) != (sections is not None):
         raise ValueError("positions of three axes come with the pairs of each in sections")
     if sections is not None and (positions is None or len(sections) != 3):
         raise ValueError("sections are three numbers, and come with positions [3, rows]")
-    args = StageAppendArgs(
-        device, _batch(batch, device), cache, rows, q_out.shape[1], qkv.data_ptr(), q_out.data_ptr(),
+    args = _APPEND.pack(
+        device, _batch(batch, device), *cache, rows, hq, qkv.data_ptr(), q_out.data_ptr(),
         _row_stride(qkv, "qkv", device), _row_stride(q_out, "q_out", device), _type(qkv), _type(q_out),
         _plain(q_gain, "q_gain", torch.bfloat16, (d,), device), _plain(k_gain, "k_gain", torch.bfloat16, (d,), device),
-        eps, cos.shape[0], _plain(cos, "cos", torch.float32, (None, d // 2), device),
-        _plain(sin, "sin", torch.float32, (cos.shape[0], d // 2), device),
+        eps, angles, _plain(cos, "cos", torch.float32, (angles, d // 2), device),
+        _plain(sin, "sin", torch.float32, (angles, d // 2), device),
         _plain(positions, "positions", torch.int32, (rows,) if axes == 1 else (3, rows), device), axes,
-        (c_int32 * 3)(*(sections or (d // 2, 0, 0))))
+        *(sections or (d // 2, 0, 0)))
     if rows:
-        _check(lib().stage_norm_rope_append(ctypes.byref(args), _handle(stream, device)))
+        rc = lib().stage_norm_rope_append(args, _handle(stream, device))
+        if rc:
+            _check(rc)
     return q_out
 
 
 def _window_args(q, out, pool, batch, window, sinks, scale):
     device = _device(q)
     cache = _cache(pool, device)
-    if q.dim() != 3 or q.shape != out.shape or q.dtype != out.dtype or q.shape[2] != cache.head_dim:
+    shape = q.shape
+    if len(shape) != 3 or out.shape != shape or q.dtype is not out.dtype or shape[2] != cache[3]:
         raise ValueError(f"q {tuple(q.shape)} {q.dtype}, out {tuple(out.shape)} {out.dtype} and pool {tuple(pool.shape)} do not fit")
-    return device, StageWindowArgs(device, _batch(batch, device), cache, q.shape[0], q.shape[1], window, sinks, scale,
-                                   q.data_ptr(), out.data_ptr(), _row_stride(q, "q", device),
-                                   _row_stride(out, "out", device), _type(q))
+    return device, _WINDOW.pack(device, _batch(batch, device), *cache, shape[0], shape[1], window, sinks, scale,
+                                q.data_ptr(), out.data_ptr(), _row_stride(q, "q", device),
+                                _row_stride(out, "out", device), _type(q))
 
 
 def stage_window_workspace(q: torch.Tensor, out: torch.Tensor, pool: torch.Tensor, batch: StageBatch, window: int = 0,
                            sinks: int = 0) -> int:
     """Bytes of workspace that stage_window_attention takes with these arguments."""
     need = c_int64()
-    _check(lib().stage_window_workspace(ctypes.byref(_window_args(q, out, pool, batch, window, sinks, 0.0)[1]), ctypes.byref(need)))
+    _check(lib().stage_window_workspace(_window_args(q, out, pool, batch, window, sinks, 0.0)[1], ctypes.byref(need)))
     return need.value
 
 
@@ -192,20 +220,21 @@ def stage_window_attention(q: torch.Tensor, out: torch.Tensor, pool: torch.Tenso
     device, args = _window_args(q, out, pool, batch, window, sinks, scale)
     if q.shape[0]:
         L = lib()
-        ws = _workspace(L.stage_window_workspace, args, device, workspace, stream)
-        _check(L.stage_window_attention(ctypes.byref(args), None if ws is None else ws.data_ptr(),
-                                        0 if ws is None else ws.nbytes, _handle(stream, device)))
+        ws, size, keep = _workspace(L.stage_window_workspace, args, device, workspace, stream)
+        rc = L.stage_window_attention(args, ws, size, _handle(stream, device))
+        if rc:
+            _check(rc)
     return out
 
 
 def _adapter_args(x, base, out, a, b, ids, ranks, scales):
     device = _device(x)
     if x.dim() != 2 or base.dim() != 2 or base.shape != out.shape or base.shape[0] != x.shape[0] or \
-            not x.dtype == base.dtype == out.dtype or a.dim() != 3:
+            not x.dtype is base.dtype is out.dtype or a.dim() != 3:
         raise ValueError(f"x {tuple(x.shape)} {x.dtype}, base {tuple(base.shape)} {base.dtype} and out {tuple(out.shape)} "
                          f"{out.dtype} do not fit")
-    (rows, k), n, (count, rank) = x.shape, base.shape[1], a.shape[:2]
-    return device, StageAdapterArgs(
+    (rows, k), n, (count, rank, _) = x.shape, base.shape[1], a.shape
+    return device, _ADAPTER.pack(
         device, rows, k, n, count, rank, _type(x), x.data_ptr(), base.data_ptr(), out.data_ptr(),
         _row_stride(x, "x", device), _row_stride(base, "base", device), _row_stride(out, "out", device),
         _plain(a, "a", torch.bfloat16, (count, rank, k), device), _plain(b, "b", torch.bfloat16, (count, n, rank), device),
@@ -217,7 +246,7 @@ def stage_adapter_workspace(x, base, out, a, b, ids, ranks=None, scales=None) ->
     """Bytes of workspace that stage_adapter_add takes with these arguments."""
     need = c_int64()
     args = _adapter_args(x, base, out, a, b, ids, ranks, scales)[1]
-    _check(lib().stage_adapter_workspace(ctypes.byref(args), ctypes.byref(need)))
+    _check(lib().stage_adapter_workspace(args, ctypes.byref(need)))
     return need.value
 
 
@@ -229,7 +258,8 @@ def stage_adapter_add(x: torch.Tensor, base: torch.Tensor, out: torch.Tensor, a:
     device, args = _adapter_args(x, base, out, a, b, ids, ranks, scales)
     if x.shape[0]:
         L = lib()
-        ws = _workspace(L.stage_adapter_workspace, args, device, workspace, stream)
-        _check(L.stage_adapter_add(ctypes.byref(args), None if ws is None else ws.data_ptr(),
-                                   0 if ws is None else ws.nbytes, _handle(stream, device)))
+        ws, size, keep = _workspace(L.stage_adapter_workspace, args, device, workspace, stream)
+        rc = L.stage_adapter_add(args, ws, size, _handle(stream, device))
+        if rc:
+            _check(rc)
     return out

@@ -44,3 +44,29 @@ def test_tensors_of_the_host_are_refused():
         P.stage_adapter_add(x, x, x, torch.zeros(1, 4, 8).bfloat16(), torch.zeros(1, 8, 4).bfloat16(), torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
         P.stage_batch(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32), 1, 1)
+
+
+def test_packed_arguments_are_the_structs():
+    """Each field of a packed call is where the structure has it."""
+    from paper_2512_21835_amd import ops
+    assert ops._BATCH.size == ctypes.sizeof(P.StageBatch)
+    batch = P.StageBatch.from_buffer_copy(ops._BATCH.pack(*range(1, 8)))
+    assert [getattr(batch, n) for n, _ in P.StageBatch._fields_] == list(range(1, 8))
+    for packed, kind in ((ops._APPEND, P.StageAppendArgs), (ops._WINDOW, P.StageWindowArgs), (ops._ADAPTER, P.StageAdapterArgs)):
+        assert packed.size == ctypes.sizeof(kind)
+        values = list(range(11, 11 + 40))
+        args = kind.from_buffer_copy(packed.pack(*[bytes(batch) if packed is not ops._ADAPTER and i == 1 else values[i]
+                                                   for i in range(len(packed.unpack(bytes(packed.size))))]))
+        flat = []
+        for n, _ in kind._fields_:
+            v = getattr(args, n)
+            if isinstance(v, ctypes.Array):
+                flat += list(v)
+            elif isinstance(v, P.StageCache):
+                flat += [getattr(v, m) for m, _ in P.StageCache._fields_]
+            elif isinstance(v, P.StageBatch):
+                assert bytes(v) == bytes(batch)
+                flat.append(values[len(flat)])
+            else:
+                flat.append(v)
+        assert flat == values[:len(flat)]
