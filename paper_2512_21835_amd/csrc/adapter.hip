@@ -249,6 +249,7 @@ struct UpLds {   // a wavefront's: S stages of B (by the adapters' rank), S of b
     static constexpr int S = 3, E = TYPE == STAGE_F32 ? 4 : 2, Y_STAGE = kTile * kCols * E, YCOPIES = Y_STAGE / 1024;
     static constexpr int b_stage(int max_rank) { return kCols * 2 * (max_rank > 32 ? 64 : max_rank > 16 ? 32 : 16); }
     static constexpr int bytes(int max_rank) { return S * (b_stage(max_rank) + Y_STAGE); }
+    static constexpr int ZEROS = 1024;   // of the workgroup, ahead of the wavefronts'
 };
 template <int TYPE, int WAYS, int T_STEPS>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterPlan pl, int blocks_per_group) {
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
     if (n_items == 0) n_items = 1;   // (of no rank: base to out)
     const bool any = __builtin_amdgcn_ballot_w64(write) != 0, wide = R % 8 == 0;
     const int n_blocks = (a.n + kCols - 1) / kCols, end = min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
-    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * L::bytes(R);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + L::ZEROS + wave * L::bytes(R);
     const uint32_t y_ring = ring + S * b_stage;
 
     struct Place { int nb, slot, item, ranks, copies; };   // block and its place in y_ring, item, its ranks, its copies
@@ -297,35 +298,72 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
     };
     // log2 of the 16-byte chunks that the item's rows have in LDS: 2, 4 or 8
     auto log_chunks = [](int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 3; };
+    // whether they are all of the adapter's ranks
+    auto exact = [](int ranks) { return (ranks == 16) | (ranks == 32) | (ranks >= 64); };
     // chunk c of row r lies at c ^ place(r): every 16 lanes of a fragment's read meet distinct banks (two chunks: pairs)
     auto place = [](int r, int lc) { return ((r & 3) | (r >> 4 & 3) << 2) >> (4 - lc); };
     auto y_place = [](int r) { return YCH == 16 ? r : r >> 1; };   // (likewise, of 16 rows of base)
+    // where instruction i of base's copies reads, for a whole block
+    uint32_t y_from[YCOPIES];
+#pragma unroll
+    for (int i = 0; i < YCOPIES; ++i) {
+        const int e = 64 * i + lane, r = e / YCH, c = (e % YCH) ^ y_place(r);
+        y_from[i] = E * (uint32_t)min(r, a.rows - 1 - row0) * (uint32_t)a.base_ld + 16 * c;
+    }
+    // copies of B for whole blocks of all ranks: instruction i has rows (64 >> LC) i + lane / 2^LC, of which place() takes
+    // i (LC 1, 2) or lane / 16 % 2 and i / 2 (LC 3)
+    auto copy_whole = [&](auto log, const uint16_t *w, uint32_t at) {
+        constexpr int LC = decltype(log)::value;
+        const uint32_t rows = 2 * (uint32_t)(lane >> LC) * R;
+        const uint32_t c = 16 * ((lane & ((1 << LC) - 1)) ^ (LC == 3 ? lane >> 4 & 1 : 0));
+#pragma unroll
+        for (int i = 0; i < 1 << LC; ++i)
+            dma16((c ^ (16 * (LC == 3 ? i / 2 * 2 : i))) + rows, w + (size_t)i * (64 >> LC) * R, at + 1024 * i);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Three = std::integral_constant<int, 3>;
     auto copy = [&](Place &p, uint32_t at) {
         p.copies = 0;
         if (p.nb >= end) return;
-        if (p.item == 0) {   // base: rows past the last: that one; columns past the last: the first
+        const bool whole = kCols * (p.nb + 1) <= a.n;
+        if (p.item == 0) {
             p.copies = YCOPIES;
             const char *const from = static_cast<const char *>(a.base) + E * ((size_t)row0 * a.base_ld + (size_t)kCols * p.nb);
 #pragma unroll
             for (int i = 0; i < YCOPIES; ++i) {
-                const int e = 64 * i + lane, r = e / YCH, c = ((e % YCH) ^ y_place(r)) * (16 / E);
-                dma16(E * ((uint32_t)min(r, a.rows - 1 - row0) * (uint32_t)a.base_ld + (kCols * p.nb + c < a.n ? c : 0)), from,
-                      y_ring + (p.slot * YCOPIES + i) * 1024);
+                uint32_t y = y_from[i];
+                if (!whole) {   // columns past the last: the first
+                    const int e = 64 * i + lane, c = ((e % YCH) ^ y_place(e / YCH)) * (16 / E);
+                    if (kCols * p.nb + c >= a.n) y -= E * c;
+                }
+                dma16(y, from, y_ring + (p.slot * YCOPIES + i) * 1024);
             }
         }
         if (p.ranks == 0 || !wide) return;
         const int lc = log_chunks(p.ranks), n = 1 << lc;
         p.copies += n;
         const uint16_t *const w = uniform(item_b, p.item) + (size_t)kCols * p.nb * R;
+        if (whole & exact(p.ranks)) {
+            if (lc == 3) copy_whole(Three{}, w, at);
+            else if (lc == 2) copy_whole(Two{}, w, at);
+            else copy_whole(One{}, w, at);
+            return;
+        }
         const int last = a.n - 1 - kCols * p.nb;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (i >= n) break;
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
             const int e = 64 * i + lane, r = e >> lc, c = (e & ((1 << lc) - 1)) ^ place(r, lc);
             // (rows past the last column: that one; chunks past the rank: the first, cut below)
             dma16(2 * ((uint32_t)min(r, last) * R + (8 * c < p.ranks ? 8 * c : 0)), w, at + 1024 * i);
         }
     };
+    // the fragments' first addresses: row 16 (l16 / 4) + l16 % 4, chunk lq (of two: lanes past them read zeros)
+    const uint32_t zeros = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    for (int i = threadIdx.x; i < L::ZEROS / 4; i += 256) reinterpret_cast<int *>(lds)[i] = 0;
+    const int fr = 16 * (l16 >> 2) + (l16 & 3);
+    auto frag_from = [&](int lc) { return (uint32_t)(16 * ((fr << lc) + ((lq & ((1 << lc) - 1)) ^ place(fr, lc)))); };
+    const uint32_t from1 = frag_from(1), from2 = frag_from(2), from3 = frag_from(3);
     Place p0{(int)blockIdx.x * blocks_per_group + wave / WAYS, 0, 0, 0, 0};
     fill(p0);
     copy(p0, ring);
@@ -364,6 +402,8 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
         for (int j = 0; j < 8; ++j) v[j] = j0 + j < t.rank ? v[j] * scale : 0.f;
         split_terms8<3>(v, x[s]);
     }
+    wait_lgkm<0>();
+    lds_barrier();   // (the zeros)
     f32x4_t d[4], sum[4];   // of the adapter; of the row's adapter
     int stores1 = 0, stores2 = 0, first_step = 0;   // stores of the turn before, and of the one before that
     uint32_t at = ring;
@@ -377,19 +417,35 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
         asm volatile("" ::: "memory");
         stores2 = stores1;
         stores1 = 0;
-        const int id = __builtin_amdgcn_readlane(item_id, p0.item), lc = log_chunks(p0.ranks);
+        const int id = __builtin_amdgcn_readlane(item_id, p0.item);
         u32x4 f[2][4];
+        if (!wide) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int r = 16 * (l16 >> 2) + 4 * m + (l16 & 3), c = 4 * e + lq;
-                f[e][m] = u32x4{0, 0, 0, 0};
-                if (kStep * e >= p0.ranks) continue;
-                if (wide) f[e][m] = *(lds16)(at + 16 * ((r << lc) + ((c & ((1 << lc) - 1)) ^ place(r, lc))));
-                else f[e][m] = load_ranks(uniform(item_b, p0.item) + (size_t)min(kCols * p0.nb + r, a.n - 1) * R, 8 * c, p0.ranks);
-                if (kStep * (e + 1) > p0.ranks) f[e][m] = cut_ranks(f[e][m], kStep * e + 8 * lq, p0.ranks);
-            }
+                for (int m = 0; m < 4; ++m) {
+                    f[e][m] = u32x4{0, 0, 0, 0};
+                    if (kStep * e < p0.ranks)
+                        f[e][m] = load_ranks(uniform(item_b, p0.item) + (size_t)min(kCols * p0.nb + fr + 4 * m, a.n - 1) * R, kStep * e + 8 * lq, p0.ranks);
+                }
+        } else if (p0.ranks > 32) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) f[e][m] = *(lds16)(at + (from3 ^ 64 * e) + 512 * m);
+        } else {
+            const uint32_t from = p0.ranks > 16 ? at + from2 : lq < 2 ? at + from1 : zeros;
+            const uint32_t by = p0.ranks > 16 ? 256 : 128;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) f[0][m] = *(lds16)(from + by * m);
+        }
+        if (!wide | !exact(p0.ranks)) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    if (kStep * e < p0.ranks) f[e][m] = cut_ranks(f[e][m], kStep * e + 8 * lq, p0.ranks);
+        }
         if (first_step == 0) {
 #pragma unroll
             for (int m = 0; m < 4; ++m) d[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -462,7 +518,7 @@ AdapterPlan adapter_plan(const AdapterArgs &a) {
 
 template <int TYPE>
 hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles, hipStream_t st) {
-    const int blocks = (a.n + kCols - 1) / kCols, lds = 4 * UpLds<TYPE>::bytes(a.max_rank);
+    const int blocks = (a.n + kCols - 1) / kCols, lds = UpLds<TYPE>::ZEROS + 4 * UpLds<TYPE>::bytes(a.max_rank);
     const long want = (long)(160 * 1024 / lds) * device_compute_units();   // workgroups: as many as run at once
     // few tiles: the wavefronts share a block's adapters; many: a block each
     const bool shared = p.groups > 1 && a.n_adapters >= 4;
@@ -472,9 +528,6 @@ hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles,
     const dim3 grid((unsigned)((blocks + per - 1) / per), tiles);
     auto launch = [&](auto ways, auto steps) -> hipError_t {
         auto *const kernel = adapter_up_kernel<TYPE, decltype(ways)::value, decltype(steps)::value>;
-        // (more LDS than a launch may take unasked)
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
         STG_LAUNCH(kernel, grid, dim3(256), lds, st, a, p, (int)per);
         return hipGetLastError();
     };

@@ -36,12 +36,13 @@ bool pointers_ok(const stage_batch &b, const stage_cache &c) {
 }
 
 bool device_ok(int device) {
-    int n = 0;
-    if (hipGetDeviceCount(&n) != hipSuccess) {
+    static const int count = [] {   // (devices do not come and go while a process runs)
+        int n = 0;
+        if (hipGetDeviceCount(&n) == hipSuccess) return n;
         (void)hipGetLastError();
-        return false;
-    }
-    return device >= 0 && device < n;
+        return 0;
+    }();
+    return device >= 0 && device < count;
 }
 
 OpRows op_rows(const stage_batch &b, const stage_cache &c, int rows) {

@@ -509,7 +509,9 @@ SplitPlan split_plan(const WindowArgs &a) {
     const long blocks = (long)a.rows.n_seqs * p.blocks_per_seq * a.n_kv_heads;
     const long groups = 2L * device_compute_units();
     const long splits = blocks >= groups ? 1 : (groups + blocks - 1) / blocks;
+    // (four pages a wavefront at least: the joining launch costs more than those take)
     p.pages = (int)((pages + 4 * splits - 1) / (4 * splits));
+    p.pages = p.pages < 4 ? 4 : p.pages;
     p.splits = (int)((pages + 4L * p.pages - 1) / (4L * p.pages));
     return p;
 }
