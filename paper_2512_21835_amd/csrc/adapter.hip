@@ -236,7 +236,7 @@ __device__ __forceinline__ void wait_most(int n) {
 }
 
 // A workgroup: a tile and blocks of 64 columns of out, a wavefront each.  A block's items are the tile's adapters, and
-// of each up to 64 ranks at a time; B's of the next two items (and base's of a block with its first) are copied into LDS
+// of each up to 64 ranks at a time; B's of the next item (and base's of a block with its first) are copied into LDS
 // while one is multiplied; the loop has no load of another kind, whose wait would take in the copies.  WAYS
 // wavefronts share the blocks, each with every WAYS-th adapter, whose rows it writes (the first also those without
 // one).  A lane has 16 neighbouring columns of a row: MFMA m's row i is column 16 (i / 4) + 4 m + i % 4 of the block.
@@ -246,10 +246,9 @@ __device__ __forceinline__ void wait_most(int n) {
 constexpr int kCols = 64, kRanks = 64;
 template <int TYPE>
 struct UpLds {   // a wavefront's: S stages of B (by the adapters' rank), S of base
-    static constexpr int S = 3, E = TYPE == STAGE_F32 ? 4 : 2, Y_STAGE = kTile * kCols * E, YCOPIES = Y_STAGE / 1024;
+    static constexpr int S = 2, E = TYPE == STAGE_F32 ? 4 : 2, Y_STAGE = kTile * kCols * E, YCOPIES = Y_STAGE / 1024;
     static constexpr int b_stage(int max_rank) { return kCols * 2 * (max_rank > 32 ? 64 : max_rank > 16 ? 32 : 16); }
     static constexpr int bytes(int max_rank) { return S * (b_stage(max_rank) + Y_STAGE); }
-    static constexpr int ZEROS = 1024;   // of the workgroup, ahead of the wavefronts'
 };
 template <int TYPE, int WAYS, int T_STEPS>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterPlan pl, int blocks_per_group) {
@@ -283,7 +282,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
     if (n_items == 0) n_items = 1;   // (of no rank: base to out)
     const bool any = __builtin_amdgcn_ballot_w64(write) != 0, wide = R % 8 == 0;
     const int n_blocks = (a.n + kCols - 1) / kCols, end = min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
-    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + L::ZEROS + wave * L::bytes(R);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * L::bytes(R);
     const uint32_t y_ring = ring + S * b_stage;
 
     struct Place { int nb, slot, item, ranks, copies; };   // block and its place in y_ring, item, its ranks, its copies
@@ -292,7 +291,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
         if (++p.item == n_items) {
             p.item = 0;
             p.nb += 4 / WAYS;
-            p.slot = p.slot == S - 1 ? 0 : p.slot + 1;
+            p.slot ^= 1;
         }
         fill(p);
     };
@@ -358,65 +357,64 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
             dma16(2 * ((uint32_t)min(r, last) * R + (8 * c < p.ranks ? 8 * c : 0)), w, at + 1024 * i);
         }
     };
-    // the fragments' first addresses: row 16 (l16 / 4) + l16 % 4, chunk lq (of two: lanes past them read zeros)
-    const uint32_t zeros = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    for (int i = threadIdx.x; i < L::ZEROS / 4; i += 256) reinterpret_cast<int *>(lds)[i] = 0;
+    // the fragments' first addresses: row 16 (l16 / 4) + l16 % 4, chunk lq
     const int fr = 16 * (l16 >> 2) + (l16 & 3);
     auto frag_from = [&](int lc) { return (uint32_t)(16 * ((fr << lc) + ((lq & ((1 << lc) - 1)) ^ place(fr, lc)))); };
     const uint32_t from1 = frag_from(1), from2 = frag_from(2), from3 = frag_from(3);
     Place p0{(int)blockIdx.x * blocks_per_group + wave / WAYS, 0, 0, 0, 0};
     fill(p0);
-    copy(p0, ring);
-    Place p1 = p0;
-    advance(p1);
-    copy(p1, ring + b_stage);
-
-    // t as operand fragments: the slices added
+    // t as operand fragments: the slices added, a row's ranks by neighbouring lanes, into LDS (where the first wavefront's
+    // second stage will be; of more ranks, where the first ones will be)
+    constexpr bool EARLY = kStep * T_STEPS <= kRanks;
+    if (EARLY) copy(p0, ring);
+    float *const t_lds = reinterpret_cast<float *>(lds + (EARLY ? b_stage : 0));
+    const int quads = R / 4, trow = R + 4;
+    for (int e = threadIdx.x; e < kTile * quads; e += 256) {
+        const int r = e / quads, j = e % quads * 4;
+        const float *const p = a.part + (size_t)min(row0 + r, a.rows - 1) * R + j;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        for (int s0 = 0; s0 < pl.slices; s0 += 8) {
+            f32x4_t u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const f32x4_t *>(p + (size_t)min(s0 + i, pl.slices - 1) * a.rows * R);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (s0 + i < pl.slices) v += u[i];
+        }
+        *reinterpret_cast<f32x4_t *>(t_lds + r * trow + j) = v;
+    }
     const float scale = a.scales && t.id >= 0 ? a.scales[t.id] : 1.f;
+    wait_lgkm<0>();
+    lds_barrier();
     bf16x8_t x[T_STEPS][3];
 #pragma unroll
     for (int s = 0; s < T_STEPS; ++s) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        float v[8];
         const int j0 = kStep * s + 8 * lq;
-        const float *const p = a.part + (size_t)min(row, a.rows - 1) * R + min(j0, R - 4);
-        const int more = j0 + 4 < R ? 4 : 0;   // (ranks that are none are read all the same, and dropped)
-        for (int s0 = 0; kStep * s < R && s0 < pl.slices; s0 += 8) {
-            f32x4_t u[8], w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const size_t at = (size_t)min(s0 + i, pl.slices - 1) * a.rows * R;
-                u[i] = *reinterpret_cast<const f32x4_t *>(p + at);
-                w[i] = *reinterpret_cast<const f32x4_t *>(p + at + more);
-            }
+        for (int h = 0; h < 8; h += 4) {
+            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(t_lds + l16 * trow + min(j0 + h, R - 4));
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (s0 + i < pl.slices) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        v[j] += u[i][j];
-                        v[4 + j] += w[i][j];
-                    }
-                }
+            for (int j = 0; j < 4; ++j) v[h + j] = j0 + h + j < t.rank ? u[j] * scale : 0.f;   // (others' are not looked at)
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j0 + j < t.rank ? v[j] * scale : 0.f;
         split_terms8<3>(v, x[s]);
     }
     wait_lgkm<0>();
-    lds_barrier();   // (the zeros)
+    lds_barrier();
+    if (!EARLY) copy(p0, ring);
     f32x4_t d[4], sum[4];   // of the adapter; of the row's adapter
-    int stores1 = 0, stores2 = 0, first_step = 0;   // stores of the turn before, and of the one before that
+    int stores = 0, first_step = 0;   // stores of the turn before, behind the copies of p0's
     uint32_t at = ring;
     while (p0.nb < end) {
-        Place p2 = p1;
-        advance(p2);
-        wait_lgkm<0>();   // the stage's last readers are done
+        Place p1 = p0;
+        advance(p1);
+        const uint32_t other = at == ring ? ring + b_stage : ring;
+        wait_lgkm<0>();   // its last readers are done
         asm volatile("" ::: "memory");
-        copy(p2, at == ring ? ring + 2 * b_stage : at - b_stage);
-        wait_most(p1.copies + p2.copies + stores1 + stores2);
+        copy(p1, other);
+        wait_most(p1.copies + stores);
         asm volatile("" ::: "memory");
-        stores2 = stores1;
-        stores1 = 0;
+        stores = 0;
         const int id = __builtin_amdgcn_readlane(item_id, p0.item);
         u32x4 f[2][4];
         if (!wide) {
@@ -434,10 +432,10 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
 #pragma unroll
                 for (int m = 0; m < 4; ++m) f[e][m] = *(lds16)(at + (from3 ^ 64 * e) + 512 * m);
         } else {
-            const uint32_t from = p0.ranks > 16 ? at + from2 : lq < 2 ? at + from1 : zeros;
-            const uint32_t by = p0.ranks > 16 ? 256 : 128;
+            const uint32_t from = at + (p0.ranks > 16 ? from2 : from1), by = p0.ranks > 16 ? 256 : 128;
+            const uint32_t keep = p0.ranks > 16 || lq < 2 ? ~0u : 0u;   // (of two chunks, for the lanes that have them)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) f[0][m] = *(lds16)(from + by * m);
+            for (int m = 0; m < 4; ++m) f[0][m] = *(lds16)(from + by * m) & u32x4{keep, keep, keep, keep};
         }
         if (!wide | !exact(p0.ranks)) {
 #pragma unroll
@@ -470,7 +468,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
             for (int m = 0; m < 4; ++m) sum[m] = d[m];
         }
         if (p1.nb != p0.nb) {   // the block's last
-            if (any) stores1 = E;
+            if (any) stores = E;
             const int c0 = kCols * p0.nb + 16 * lq;
             if (write && c0 < a.n) {
                 const uint32_t from = y_ring + p0.slot * L::Y_STAGE + l16 * (16 * YCH);
@@ -498,8 +496,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
             }
         }
         p0 = p1;
-        p1 = p2;
-        at = at == ring + 2 * b_stage ? ring : at + b_stage;
+        at = other;
     }
 }
 
@@ -518,7 +515,7 @@ AdapterPlan adapter_plan(const AdapterArgs &a) {
 
 template <int TYPE>
 hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles, hipStream_t st) {
-    const int blocks = (a.n + kCols - 1) / kCols, lds = UpLds<TYPE>::ZEROS + 4 * UpLds<TYPE>::bytes(a.max_rank);
+    const int blocks = (a.n + kCols - 1) / kCols, lds = 4 * UpLds<TYPE>::bytes(a.max_rank);
     const long want = (long)(160 * 1024 / lds) * device_compute_units();   // workgroups: as many as run at once
     // few tiles: the wavefronts share a block's adapters; many: a block each
     const bool shared = p.groups > 1 && a.n_adapters >= 4;
