@@ -516,7 +516,7 @@ AdapterPlan adapter_plan(const AdapterArgs &a) {
 template <int TYPE>
 hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles, hipStream_t st) {
     const int blocks = (a.n + kCols - 1) / kCols, lds = 4 * UpLds<TYPE>::bytes(a.max_rank);
-    const long want = (long)(160 * 1024 / lds) * device_compute_units();   // workgroups: as many as run at once
+    const long want = (lds > 80 * 1024 ? 1L : 2L) * device_compute_units();   // workgroups: as many as run at once
     // few tiles: the wavefronts share a block's adapters; many: a block each
     const bool shared = p.groups > 1 && a.n_adapters >= 4;
     const int least = shared ? 1 : 4;
