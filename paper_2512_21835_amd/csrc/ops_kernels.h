@@ -85,6 +85,7 @@ struct WindowArgs {
 // Bytes of WindowArgs::part that a call takes (it looks at the sizes only).
 size_t window_workspace(const WindowArgs &a);
 hipError_t launch_window_attention(const WindowArgs &a, hipStream_t st);
+hipError_t launch_window_f32(const WindowArgs &a, hipStream_t st);   // its prompts over an fp32 cache
 
 struct AdapterArgs {
     const void *x, *base;

@@ -8,52 +8,11 @@
 // over workgroups and their wavefronts, states joined at the end (window_merge where the workgroups are several).
 #include <type_traits>
 
-#include "lanes.h"
 #include "lds_dma.h"
-#include "ops_kernels.h"
-#include "stage_ops.h"
+#include "window_rows.h"
 
 namespace stg {
 namespace {
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef const __attribute__((address_space(4))) int *const_ints;
-typedef __attribute__((address_space(3))) u32x4 *lds16;
-typedef __attribute__((address_space(3))) s16x4_t *lds8;
-typedef __attribute__((address_space(3))) float *lds4;
-
-constexpr int kPage = kBlockTokens;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.f;
-
-// The same in every lane, and known to be.
-__device__ __forceinline__ OpRows::Seq uniform(OpRows::Seq s) {
-    const uint64_t t = (uint64_t)(uintptr_t)s.table;
-    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)t), high = __builtin_amdgcn_readfirstlane((uint32_t)(t >> 32));
-    return {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.pos0),
-            reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low))};
-}
-
-// Inclusive sums over the lanes (DPP: within rows of 16, then row to row).
-__device__ __forceinline__ int lane_scan(int v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast 15: rows 0, 2 to 1, 3
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast 31: row 1 to 2 and 3
-    return v;
-}
-__device__ __forceinline__ const int *lane_pointer(const int *p, int lane) {
-    const uint64_t t = (uint64_t)(uintptr_t)p;
-    const uint32_t low = __builtin_amdgcn_readlane((uint32_t)t, lane), high = __builtin_amdgcn_readlane((uint32_t)(t >> 32), lane);
-    return reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low));
-}
 
 // The pages that rows at positions first .. last see: pages 0 .. sink - 1, then from, from + 1, ...; n in all.
 struct Span {
@@ -70,52 +29,6 @@ __device__ __forceinline__ Span span_of(const WindowArgs &a, int first, int last
     if (s.end <= 0) s.n = 0;
     return s;
 }
-__device__ __forceinline__ bool sees(const WindowArgs &a, int pos, int key) {
-    return (key <= pos) & (key < a.rows.max_len) & ((key > pos - a.window) | (key < a.sinks));   // (no branches)
-}
-// Whether rows at positions first .. last all see keys k0 .. k0 + n - 1.
-__device__ __forceinline__ bool all_see(const WindowArgs &a, int first, int last, int k0, int n) {
-    return k0 + n - 1 <= first && k0 + n <= a.rows.max_len && (k0 > last - a.window || k0 + n <= a.sinks);
-}
-
-__device__ __forceinline__ float load_elem(const void *p, size_t e, int type) {
-    if (type == STAGE_F32) return static_cast<const float *>(p)[e];
-    return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[e] << 16);
-}
-__device__ __forceinline__ void load4(const void *p, size_t e, int type, float v[4]) {
-    if (type == STAGE_F32) {
-        const float4 x = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e);
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-    } else {
-        const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + e);
-        v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ void store4(void *p, size_t e, int type, float4 v) {
-    if (type == STAGE_F32) {
-        *reinterpret_cast<float4 *>(static_cast<float *>(p) + e) = v;
-    } else {
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(p) + e) = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
-    }
-}
-// o / l; a row that saw no key is 0.
-__device__ __forceinline__ float4 quotient(float4 o, float l) {
-    const float r = l == 0.f ? 0.f : 1.f / l;
-    return make_float4(o.x * r, o.y * r, o.z * r, o.w * r);
-}
-
-// Term t of x as a sum of bf16 terms, each the nearest to what the ones before leave: three terms hold all 24 bits.
-template <int TERMS>
-__device__ __forceinline__ void split_terms(float x, __bf16 t[TERMS]) {
-#pragma unroll
-    for (int i = 0; i < TERMS; ++i) {
-        t[i] = (__bf16)x;
-        x -= (float)t[i];
-    }
-}
-
 // The LDS image of a cache page: K rows, then V rows, as they lie in the cache, with the 16-byte chunks of each row
 // permuted (by the copies' lane addresses) so that the fragments' reads meet distinct banks.
 template <int D, bool F32>
@@ -573,30 +486,10 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, log_bq = (CB == 1 ? 7 : 8) - pl.log_g, bq = 1 << log_bq;
-    // the sequence and the block of its rows: blocks of all sequences in turn, 64 sequences at a time
-    int block = blockIdx.x / hkv;
-    OpRows::Seq seq;
-    for (int i0 = 0;; i0 += 64) {
-        if (i0 >= a.rows.n_seqs) return;
-        const int i = min(i0 + lane, a.rows.n_seqs - 1);
-        OpRows::Seq at = a.rows.seq(i);
-        const int own = i0 + lane < a.rows.n_seqs ? (min(at.n, a.rows.max_rows) + bq - 1) >> log_bq : 0, sum = lane_scan(own);
-        const int before = __popcll(__builtin_amdgcn_ballot_w64(sum <= block));   // (sums ascend)
-        if (before < 64) {
-            // the last rows, which see the most keys, first
-            block = __builtin_amdgcn_readlane(sum, before) - 1 - block;
-            seq = {__builtin_amdgcn_readlane(at.first, before), __builtin_amdgcn_readlane(at.n, before),
-                   __builtin_amdgcn_readlane(at.pos0, before), lane_pointer(at.table, before)};
-            break;
-        }
-        block -= __builtin_amdgcn_readlane(sum, 63);
-    }
-    const int t0 = block << log_bq, rows = min(bq, min(seq.n, a.rows.max_rows) - t0), first = seq.pos0 + t0;
-    // the tiles that some row sees: 0 .. sink - 1, then from, from + 1, ...
-    const int end = min(first + rows, a.rows.max_len), last_page = max(end - 1, 0) / kPage;
-    const int sink = (max(0, min(a.sinks, end)) + KT - 1) / KT, from = max(max(0, first - a.window + 1) / KT, sink);
-    const int n_tiles = end <= 0 ? 0 : sink + max(0, (end + KT - 1) / KT - from);
-    auto tile_at = [&](int t) { return t < sink ? t : from + t - sink; };
+    RowBlock rb;
+    if (!rb.find(a, blockIdx.x / hkv, log_bq)) return;
+    const OpRows::Seq &seq = rb.seq;
+    const int t0 = rb.t0, rows = rb.rows, first = rb.first, n_tiles = rb.n_tiles, last_page = rb.last_page;
 
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const size_t head = (size_t)kPage * L::ROW, block_bytes = (size_t)2 * hkv * head;
@@ -604,8 +497,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     auto known = [&](int b) { return (unsigned)b < (unsigned)a.rows.n_blocks; };
     // Block ids of the tiles' pages, 64 (32 tiles) in a register of the wavefront, the next 64 under way: loads by
     // the scalar unit would have every wait for LDS wait for them, too.
-    auto page_at = [&](int t, int h) { return min(2 * tile_at(t) + h, last_page); };
-    auto ids_from = [&](int t) { return seq.table[page_at(t + lane / 2, lane & 1)]; };
+    auto ids_from = [&](int t) { return seq.table[rb.page_at(t + lane / 2, lane & 1)]; };
     int ids = 0, more_ids = 0;
     if (n_tiles > 0) {
         ids = ids_from(0);
@@ -677,31 +569,8 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     const uint32_t k_at = ring + col * L::ROW + 16 * (half ^ L::kx(col));   // chunk 2 kk + half of key col, permuted
     const int vk = 4 * half + (lane & 15) / 4;
     const uint32_t v_at = ring + L::HALF + vk * L::ROW + 8 * (lane & 1) + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ L::vx(vk));
-    // Turns t as ranges: below `low`, or of [from, from + n).  (Scalar work counts: a turn has few hundred cycles.)
-    struct Turns {
-        int low, from;
-        unsigned n;
-        __device__ __forceinline__ bool has(int t) const { return (t < low) | ((unsigned)(t - from) < n); }
-    };
-    // tiles that rows at positions r0 .. r1 (r0 <= r1) all see, and those with a key that some of them sees
-    auto whole = [&](int r0, int r1) {
-        Turns w;
-        w.low = min(sink, max(0, min(min(a.sinks, r0 + 1), a.rows.max_len)) / KT);
-        w.from = sink + max(0, max(0, r1 - a.window + KT) / KT - from);
-        w.n = max(0, sink + max(0, min(r0 + 1, a.rows.max_len)) / KT - from - w.from);
-        return w;
-    };
-    auto touched = [&](int r0, int r1) {   // from a turn before to a turn behind: what a wavefront takes part in
-        Turns w;
-        w.low = min(sink, (max(0, min(min(a.sinks, r1 + 1), a.rows.max_len)) + KT - 1) / KT);
-        if (w.low > 0) ++w.low;
-        w.from = sink + max(0, max(0, r0 - a.window + 1) / KT - from) - 1;
-        const int end = sink + (max(0, min(r1 + 1, a.rows.max_len)) + KT - 1) / KT - from;
-        w.n = end > w.from + 1 ? end + 1 - w.from : 0;
-        return w;
-    };
-    const Turns clear = whole(first, first + rows - 1), my_clear = whole(w_first, max(w_first, w_last));
-    Turns mine = touched(w_first, max(w_first, w_last));
+    const Turns clear = rb.whole(a, first, first + rows - 1), my_clear = rb.whole(a, w_first, max(w_first, w_last));
+    Turns mine = widened(rb.touched(a, w_first, max(w_first, w_last)));   // what the wavefront takes part in
     if (w_rows <= 0) mine = Turns{0, 0, 0};
     // This wavefront's share of tile t has landed; with the barrier behind it, everybody's.  In a tile that not every
     // row sees, a V that is not finite must not meet the matrix instructions (0 x inf): it becomes 0 here, and is
@@ -722,24 +591,13 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
         }
     };
-    // Bits 0 .. n of a word.
-    auto bits_to = [](int n) { return n < 0 ? 0u : ~0u >> (31 - min(n, 31)); };
     auto hide = [&](f32x16_t(&s)[CB], int t) {
-        const int k0 = tile_at(t) * KT + 4 * half;   // the lane's first key; its others are 8 (i / 4) + i % 4 further
+        const int k0 = rb.tile_at(t) * KT + 4 * half;   // the lane's first key; its others are 8 (i / 4) + i % 4 further
         uint32_t pages = t < n_tiles ? ~0u : 0u;
         if (strange && t < n_tiles)
-            pages = (known(seq.table[page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[page_at(t, 1)]) ? 0xFFFF0000u : 0u);
-        pages >>= 4 * half;
+            pages = (known(seq.table[rb.page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[rb.page_at(t, 1)]) ? 0xFFFF0000u : 0u);
 #pragma unroll
-        for (int x = 0; x < CB; ++x) {   // (sees(), for 32 keys at once)
-            const uint32_t seen = pages & bits_to(min(pos[x], a.rows.max_len - 1) - k0) &
-                                  (~bits_to(pos[x] - a.window - k0) | bits_to(a.sinks - 1 - k0));
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t yes = (uint32_t)((int)(seen << (31 - 8 * (i / 4) - i % 4)) >> 31);
-                s[x][i] = __uint_as_float((__float_as_uint(s[x][i]) & yes) | (0xFF800000u & ~yes));
-            }
-        }
+        for (int x = 0; x < CB; ++x) hide_scores(s[x], pages >> (4 * half) & seen_bits(a, pos[x], k0));
     };
     auto value_frag = [&](uint32_t v, int h, int b) {
         const uint32_t at = (v ^ (64 * b)) + 16 * h * L::ROW;
@@ -933,7 +791,7 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         const char *const gk = pool + 16 * half, *const gv = pool + hkv * head + 8 * half;
 #pragma unroll 1
         for (int key = 0; key < n_tiles * KT; ++key) {
-            const int t = key / KT, k0 = tile_at(t) * KT, at = k0 + key % KT, page = at / kPage;
+            const int t = key / KT, k0 = rb.tile_at(t) * KT, at = k0 + key % KT, page = at / kPage;
             if (page > last_page) continue;
             const int b = ((const_ints)(uintptr_t)seq.table)[page];
             if (!known(b) || (clear.has(t) && !strange)) continue;
@@ -1005,9 +863,7 @@ hipError_t launch_tiles(const WindowArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-bool by_tiles(const WindowArgs &a) {
-    return a.kv_type == STAGE_BF16 && a.rows.max_rows * (a.n_q_heads / a.n_kv_heads) > 16;
-}
+bool by_tiles(const WindowArgs &a) { return a.rows.max_rows * (a.n_q_heads / a.n_kv_heads) > 16; }
 
 }  // namespace
 
@@ -1020,6 +876,7 @@ size_t window_workspace(const WindowArgs &a) {
 hipError_t launch_window_attention(const WindowArgs &a, hipStream_t st) {
     if (a.rows.rows <= 0) return hipSuccess;
     const bool f32 = a.kv_type == STAGE_F32, exact = a.type == STAGE_F32;
+    if (f32 && by_tiles(a)) return launch_window_f32(a, st);
 #define STG_WINDOW_CASE(D)                                                 \
     if (a.head_dim == D && by_tiles(a))                                    \
         return exact ? launch_tiles<D, 3, 1>(a, st) : launch_tiles<D, 1, 1>(a, st); \

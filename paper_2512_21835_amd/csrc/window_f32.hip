@@ -1,0 +1,317 @@
+// Window attention of prompts over an fp32 cache.
+#include <hip/hip_runtime.h>
+
+#include "lds_dma.h"
+#include "window_rows.h"
+
+namespace stg {
+namespace {
+
+// A workgroup: 128 columns = G heads x BQ = 128 / G consecutive rows of one sequence, one KV head; wavefront w the
+// columns 32 w .. 32 w + 31 (column r: head r / BQ, row r % BQ).  K and V come in tiles of 32 keys (two pages): fp32 into
+// registers a tile ahead, from there as PL bf16 planes, whose sum they are, into one of two LDS stages.  S^T = K Q^T and
+// O^T += V^T P^T with 32x32x16 MFMAs, lane l holding keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for column l % 32, the
+// k order of the operand P^T.
+//
+// fp32 rows: three terms of q and p against three planes hold all 24 bits of each; of the nine products the six whose terms are
+// 2^-16 of the largest or more are taken, which leaves 2^-24 each.  bf16 rows: q is its one term, p one rounding to bf16
+// (2^-9 of a probability, as everywhere with bf16 rows) and two planes, 2^-17, are well below that.
+template <int D, int PL>
+struct PlaneLds {
+    static constexpr int ROW = 2 * D, HALF = kTileKeys * ROW, PLANE = 2 * HALF, BYTES = PL * PLANE;   // K and V of a plane
+    static constexpr int CHUNKS = D / 64;   // chunks of 8 elements per thread: key tid / 8, chunks tid % 8 + 8 i
+    __device__ static int kx(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
+    __device__ static int vx(int key) { return D == 128 ? (key & 3) << 2 : (key & 2) << 1; }
+};
+
+// Beyond this a number is no sum of finite bf16 terms.
+constexpr float kLargest = 0x1.FEp127f;
+
+template <int D, int TERMS, int PL>
+__global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log_g) {
+    using L = PlaneLds<D, PL>;
+    constexpr int KK = D / 16, NB = D / 32, TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32;
+    __shared__ __align__(1024) char lds[2 * L::BYTES];
+    __shared__ int flags[4];
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, log_bq = 7 - log_g, bq = 1 << log_bq;
+    RowBlock rb;
+    if (!rb.find(a, blockIdx.x / hkv, log_bq)) return;
+    const OpRows::Seq &seq = rb.seq;
+    const int t0 = rb.t0, rows = rb.rows, first = rb.first, n_tiles = rb.n_tiles;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const size_t head = (size_t)kPage * D, block_elems = (size_t)2 * hkv * head;
+    const float *const pool = static_cast<const float *>(a.pool) + g * head;
+    auto known = [&](int b) { return (unsigned)b < (unsigned)a.rows.n_blocks; };
+    // block ids of the tiles' pages: 64 (32 tiles) in a register of the wavefront, the next 64 under way
+    auto ids_from = [&](int t) { return seq.table[rb.page_at(t + lane / 2, lane & 1)]; };
+    int ids = 0, more_ids = 0;
+    if (n_tiles > 0) {
+        ids = ids_from(0);
+        more_ids = ids_from(32);
+    }
+    bool strange = __builtin_amdgcn_ballot_w64(!known(ids)) != 0;   // some page so far is not of the pool
+
+    // The thread's part of a tile: key 8 wave + lane / 8, chunks lane % 8 + 8 i of K and of V.
+    f32x4_t raw[2][L::CHUNKS][2];
+    auto fetch = [&](int t) {   // (t ascending, each once)
+        if (t > 0 && t % 32 == 0) {
+            ids = more_ids;
+            strange |= __builtin_amdgcn_ballot_w64(!known(ids)) != 0;
+            more_ids = ids_from(t + 32);
+        }
+        const int b = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
+        const float *from = pool + (size_t)(known(b) ? b : 0) * block_elems + ((wave & 1) * 8 + lane / 8) * D + lane % 8 * 8;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int i = 0; i < L::CHUNKS; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    raw[kv][i][h] = *reinterpret_cast<const f32x4_t *>(from + kv * hkv * head + 64 * i + 4 * h);
+    };
+    // A K or V that is not finite, or too large for terms, becomes 0: the columns that see it are taken again at the end.
+    bool odd = false;
+    const int my_key = 8 * wave + lane / 8;
+    const uint32_t k_to = base + my_key * L::ROW + 16 * (lane % 8 ^ L::kx(my_key));
+    const uint32_t v_to = base + L::HALF + my_key * L::ROW + 16 * (lane % 8 ^ L::vx(my_key));
+    bf16x8_t planes[PL];
+    constexpr int PIECES = 2 * L::CHUNKS * 4;   // two elements each
+    auto convert = [&](uint32_t stage, int piece) {
+        const int kv = piece / (4 * L::CHUNKS), i = piece / 4 % L::CHUNKS, e0 = piece % 4 * 2;
+#pragma unroll
+        for (int e = e0; e < e0 + 2; ++e) {
+            float x = raw[kv][i][e / 4][e % 4];
+            const bool bad = !(fabsf(x) <= kLargest);
+            odd |= bad;
+            x = bad ? 0.f : x;
+            __bf16 terms[PL];
+            split_terms<PL>(x, terms);
+#pragma unroll
+            for (int p = 0; p < PL; ++p) planes[p][e] = terms[p];
+        }
+        if (e0 == 6) {
+#pragma unroll
+            for (int p = 0; p < PL; ++p)
+                *(lds16)(((kv ? v_to : k_to) ^ (128 * i)) + stage + p * L::PLANE) = __builtin_bit_cast(u32x4, planes[p]);
+        }
+    };
+
+    // the wavefront's columns and the rows that they have: positions w_first .. w_last
+    const int c0 = 32 * wave, r0 = bq >= 32 ? c0 & (bq - 1) : 0;
+    const int w_rows = min(bq >= 32 ? 32 : bq, rows - r0), w_first = first + r0, w_last = w_first + w_rows - 1;
+    const int r = c0 + col, row = r & (bq - 1), pos = row < rows ? first + row : -1;
+    const size_t at = (size_t)((g << log_g) + (r >> log_bq)) * D + 8 * half;
+    const size_t q_at = (size_t)(seq.first + t0 + min(row, rows - 1)) * a.q_ld + at;
+    if (n_tiles > 0) fetch(0);
+    bf16x8_t q[TERMS][KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+        float v[8];
+        load4(a.q, q_at + 16 * kk, TYPE, v);
+        load4(a.q, q_at + 16 * kk + 4, TYPE, v + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            __bf16 s[TERMS];
+            split_terms<TERMS>(a.scale < 0.f ? -v[j] : v[j], s);   // (its scores' maximum is then the largest)
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i) q[i][kk][j] = s[i];
+        }
+    }
+    f32x16_t o[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const float scale = fabsf(a.scale) * kLog2e;   // scores in base 2
+    const uint32_t k_at = base + col * L::ROW + 16 * (half ^ L::kx(col));   // chunk 2 kk + half of key col, permuted
+    const int vk = 4 * half + (lane & 15) / 4;
+    const uint32_t v_at = base + L::HALF + vk * L::ROW + 8 * (lane & 1) + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ L::vx(vk));
+    auto value_frag = [&](uint32_t v, int h, int b) {
+        const uint32_t from = (v ^ (64 * b)) + 16 * h * L::ROW;
+        const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)from);
+        const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)(from + 8 * L::ROW));
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const Turns clear = rb.whole(a, w_first, max(w_first, w_last));
+    Turns mine = rb.touched(a, w_first, max(w_first, w_last));
+    if (w_rows <= 0) mine = Turns{0, 0, 0};
+
+    if (n_tiles > 0) {
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) convert(0, e);
+        if (n_tiles > 1) fetch(1);
+    }
+    for (int t = 0; t < n_tiles; ++t) {
+        // Tile t is in its stage; the other one, which tile t - 1 was read from, takes tile t + 1.
+        wait_lgkm<0>();
+        lds_barrier();
+        const uint32_t now = (t & 1) * L::BYTES, next = L::BYTES - now;
+        if (!mine.has(t)) {
+            if (t + 1 < n_tiles) {
+#pragma unroll
+                for (int e = 0; e < PIECES; ++e) convert(next, e);
+                if (t + 2 < n_tiles) fetch(t + 2);
+            }
+            continue;
+        }
+        f32x16_t s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        // (behind the last tile: what the registers hold goes to a stage that nobody reads)
+        constexpr int N = PL * KK;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const int kk = c / PL, p = PL - 1 - c % PL;   // (small terms first)
+            const bf16x8_t k = __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + now + p * L::PLANE) ^ (32 * kk)));
+#pragma unroll
+            for (int i = TERMS - 1; i >= 0; --i)
+                if (i + p < PL) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][kk], s, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e)
+                if (e * N / PIECES == c) convert(next, e);
+        }
+        if (t + 2 < n_tiles) fetch(t + 2);
+        if (!clear.has(t) | strange) {
+            uint32_t pages = ~0u;
+            if (strange)
+                pages = (known(seq.table[rb.page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[rb.page_at(t, 1)]) ? 0xFFFF0000u : 0u);
+            hide_scores(s, pages >> (4 * half) & seen_bits(a, pos, rb.tile_at(t) * kTileKeys + 4 * half));
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = fmaxf(top, lane_xor(top, 32)) * scale;
+        // a whole number that stays until a score is 2^kSlack beyond it: rescaling is exact, and rare
+        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+            const float to = top > m + kSlack ? ceilf(top) : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
+            m = to;
+            l *= alpha;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        bf16x8_t p[TERMS][2];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float w = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
+            sum += w;
+            __bf16 terms[TERMS];
+            split_terms<TERMS>(w, terms);
+#pragma unroll
+            for (int j = 0; j < TERMS; ++j) p[j][i / 8][i % 8] = terms[j];
+        }
+        l += sum;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int pl = PL - 1; pl >= 0; --pl)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const bf16x8_t v = value_frag(v_at + now + pl * L::PLANE, h, b);
+#pragma unroll
+                    for (int i = TERMS - 1; i >= 0; --i)
+                        if (i + pl < PL) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i][h], o[b], 0, 0, 0);
+                }
+    }
+    auto store = [&] {
+        const float sum = l + lane_xor(l, 32);
+        if (row < rows) {
+            const size_t to = (size_t)(seq.first + t0 + row) * a.out_ld + at - 8 * half;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    store4(a.out, to + 32 * b + 8 * j + 4 * half, TYPE,
+                           quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
+        }
+    };
+    store();
+    if (lane == 0) flags[wave] = 0;
+    if (odd) flags[wave] = 1;
+    __syncthreads();
+    if (!(flags[0] | flags[1] | flags[2] | flags[3])) return;
+    // Some K or V was cleared: the columns that see such a one again, key by key in fp32.  The others keep what they have.
+    bool again = false;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < n_tiles * kTileKeys; ++i) {
+        const int key = rb.tile_at(i / kTileKeys) * kTileKeys + i % kTileKeys;
+        if (key / kPage > rb.last_page) continue;
+        const int b = ((const_ints)(uintptr_t)seq.table)[key / kPage];
+        if (!known(b)) continue;
+        const float *const k = pool + (size_t)b * block_elems + key % kPage * D, *const v = k + hkv * head;
+        bool bad = false;
+        float w = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            float x[8], y[8];
+            load4(a.q, q_at + 16 * kk, TYPE, x);
+            load4(a.q, q_at + 16 * kk + 4, TYPE, x + 4);
+            load4(k, 16 * kk + 8 * half, STAGE_F32, y);
+            load4(k, 16 * kk + 8 * half + 4, STAGE_F32, y + 4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                bad |= !(fabsf(y[j]) <= kLargest);
+                w = fmaf(x[j], y[j], w);
+            }
+            asm volatile("" ::: "memory");   // (registers)
+        }
+        w = (w + lane_xor(w, 32)) * a.scale * kLog2e;
+        const bool seen = sees(a, pos, key);
+        const float to = seen & (w > m) ? w : m, ref = to == -INFINITY ? 0.f : to;
+        const float alpha = __builtin_amdgcn_exp2f(m - ref);
+        w = seen ? __builtin_amdgcn_exp2f(w - ref) : 0.f;
+        m = to;
+        l = l * alpha + (half ? 0.f : w);   // (the halves of a column are added up at the end)
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x[4];
+                load4(v, 32 * c + 8 * j + 4 * half, STAGE_F32, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    bad |= !(fabsf(x[e]) <= kLargest);
+                    o[c][4 * j + e] = o[c][4 * j + e] * alpha + (seen ? w * x[e] : 0.f);
+                }
+                __builtin_amdgcn_sched_barrier(0);   // (registers)
+            }
+        again |= seen & bad;
+    }
+    if (__shfl_xor((int)again, 32) | (int)again) store();
+}
+
+template <int D, int TERMS, int PL>
+hipError_t launch(const WindowArgs &a, hipStream_t st) {
+    int log_g = 0;
+    while (a.n_kv_heads << log_g < a.n_q_heads) ++log_g;
+    // row blocks: no sequence adds more than one that is not full
+    const int bq = 128 >> log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
+    const long blocks = ((long)a.rows.rows / bq + seqs) * a.n_kv_heads;
+    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    STG_LAUNCH((window_tiles_f32<D, TERMS, PL>), dim3((unsigned)blocks), dim3(256), 0, st, a, log_g);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_window_f32(const WindowArgs &a, hipStream_t st) {
+    const bool exact = a.type == STAGE_F32;
+    if (a.head_dim == 64) return exact ? launch<64, 3, 3>(a, st) : launch<64, 1, 2>(a, st);
+    if (a.head_dim == 128) return exact ? launch<128, 3, 3>(a, st) : launch<128, 1, 2>(a, st);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace stg

@@ -1,0 +1,177 @@
+// What the window attention kernels (window.hip, window_f32.hip) share: which keys a row sees, the rows of a workgroup
+// and the tiles of keys that they see, four elements of a row, numbers as sums of bf16 terms.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "lanes.h"
+#include "ops_kernels.h"
+#include "stage_ops.h"
+
+namespace stg {
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef const __attribute__((address_space(4))) int *const_ints;
+typedef __attribute__((address_space(3))) u32x4 *lds16;
+typedef __attribute__((address_space(3))) s16x4_t *lds8;
+typedef __attribute__((address_space(3))) float *lds4;
+
+constexpr int kPage = kBlockTokens;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;
+
+// The same in every lane, and known to be.
+__device__ __forceinline__ OpRows::Seq uniform(OpRows::Seq s) {
+    const uint64_t t = (uint64_t)(uintptr_t)s.table;
+    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)t), high = __builtin_amdgcn_readfirstlane((uint32_t)(t >> 32));
+    return {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.pos0),
+            reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low))};
+}
+
+// Inclusive sums over the lanes (DPP: within rows of 16, then row to row).
+__device__ __forceinline__ int lane_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast 15: rows 0, 2 to 1, 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast 31: row 1 to 2 and 3
+    return v;
+}
+__device__ __forceinline__ const int *lane_pointer(const int *p, int lane) {
+    const uint64_t t = (uint64_t)(uintptr_t)p;
+    const uint32_t low = __builtin_amdgcn_readlane((uint32_t)t, lane), high = __builtin_amdgcn_readlane((uint32_t)(t >> 32), lane);
+    return reinterpret_cast<const int *>((uintptr_t)((uint64_t)high << 32 | low));
+}
+
+__device__ __forceinline__ bool sees(const WindowArgs &a, int pos, int key) {
+    return (key <= pos) & (key < a.rows.max_len) & ((key > pos - a.window) | (key < a.sinks));   // (no branches)
+}
+// Whether rows at positions first .. last all see keys k0 .. k0 + n - 1.
+__device__ __forceinline__ bool all_see(const WindowArgs &a, int first, int last, int k0, int n) {
+    return k0 + n - 1 <= first && k0 + n <= a.rows.max_len && (k0 > last - a.window || k0 + n <= a.sinks);
+}
+
+__device__ __forceinline__ void load4(const void *p, size_t e, int type, float v[4]) {
+    if (type == STAGE_F32) {
+        const float4 x = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else {
+        const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + e);
+        v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store4(void *p, size_t e, int type, float4 v) {
+    if (type == STAGE_F32) {
+        *reinterpret_cast<float4 *>(static_cast<float *>(p) + e) = v;
+    } else {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(p) + e) = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
+    }
+}
+// o / l; a row that saw no key is 0.
+__device__ __forceinline__ float4 quotient(float4 o, float l) {
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    return make_float4(o.x * r, o.y * r, o.z * r, o.w * r);
+}
+
+// Term t of x as a sum of bf16 terms, each the nearest to what the ones before leave: three terms hold all 24 bits.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(float x, __bf16 t[TERMS]) {
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i) {
+        t[i] = (__bf16)x;
+        x -= (float)t[i];
+    }
+}
+
+// Bits 0 .. n of a word.
+__device__ __forceinline__ uint32_t bits_to(int n) { return n < 0 ? 0u : ~0u >> (31 - min(n, 31)); }
+// sees(), for the 32 keys from k0 on.
+__device__ __forceinline__ uint32_t seen_bits(const WindowArgs &a, int pos, int k0) {
+    return bits_to(min(pos, a.rows.max_len - 1) - k0) & (~bits_to(pos - a.window - k0) | bits_to(a.sinks - 1 - k0));
+}
+// -inf for the scores i whose bit 8 (i / 4) + i % 4 is not set.
+__device__ __forceinline__ void hide_scores(f32x16_t &s, uint32_t seen) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t yes = (uint32_t)((int)(seen << (31 - 8 * (i / 4) - i % 4)) >> 31);
+        s[i] = __uint_as_float((__float_as_uint(s[i]) & yes) | (0xFF800000u & ~yes));
+    }
+}
+
+// Numbers t as ranges: below `low`, or of [from, from + n).  (Scalar work counts: a turn has few hundred cycles.)
+struct Turns {
+    int low, from;
+    unsigned n;
+    __device__ __forceinline__ bool has(int t) const { return (t < low) | ((unsigned)(t - from) < n); }
+};
+
+// 2^log_bq consecutive rows of a sequence (the blocks of all sequences in turn, of each its last rows first, which see
+// the most keys), and the tiles of 32 keys that they see: 0 .. sink - 1, then from, from + 1, ...; n_tiles in all.
+constexpr int kTileKeys = 32;
+struct RowBlock {
+    OpRows::Seq seq;
+    int t0, rows, first;       // first row within the sequence, rows, position of the first
+    int end, last_page;        // keys from `end` on are seen by no row
+    int sink, from, n_tiles;
+
+    // false: there are fewer blocks
+    __device__ __forceinline__ bool find(const WindowArgs &a, int block, int log_bq) {
+        const int lane = __lane_id(), bq = 1 << log_bq;
+        for (int i0 = 0;; i0 += 64) {   // 64 sequences at a time
+            if (i0 >= a.rows.n_seqs) return false;
+            const OpRows::Seq at = a.rows.seq(min(i0 + lane, a.rows.n_seqs - 1));
+            const int own = i0 + lane < a.rows.n_seqs ? (min(at.n, a.rows.max_rows) + bq - 1) >> log_bq : 0, sum = lane_scan(own);
+            const int before = __popcll(__builtin_amdgcn_ballot_w64(sum <= block));   // (sums ascend)
+            if (before < 64) {
+                block = __builtin_amdgcn_readlane(sum, before) - 1 - block;
+                seq = {__builtin_amdgcn_readlane(at.first, before), __builtin_amdgcn_readlane(at.n, before),
+                       __builtin_amdgcn_readlane(at.pos0, before), lane_pointer(at.table, before)};
+                break;
+            }
+            block -= __builtin_amdgcn_readlane(sum, 63);
+        }
+        t0 = block << log_bq;
+        rows = min(bq, min(seq.n, a.rows.max_rows) - t0);
+        first = seq.pos0 + t0;
+        end = min(first + rows, a.rows.max_len);
+        last_page = max(end - 1, 0) / kPage;
+        sink = (max(0, min(a.sinks, end)) + kTileKeys - 1) / kTileKeys;
+        from = max(max(0, first - a.window + 1) / kTileKeys, sink);
+        n_tiles = end <= 0 ? 0 : sink + max(0, (end + kTileKeys - 1) / kTileKeys - from);
+        return true;
+    }
+    __device__ __forceinline__ int tile_at(int t) const { return t < sink ? t : from + t - sink; }
+    // page h of tile t, of those that hold a key of the sequence
+    __device__ __forceinline__ int page_at(int t, int h) const { return min(2 * tile_at(t) + h, last_page); }
+    // tiles that rows at positions r0 .. r1 (r0 <= r1) all see, and those with a key that some of them sees
+    __device__ __forceinline__ Turns whole(const WindowArgs &a, int r0, int r1) const {
+        Turns w;
+        w.low = min(sink, max(0, min(min(a.sinks, r0 + 1), a.rows.max_len)) / kTileKeys);
+        w.from = sink + max(0, max(0, r1 - a.window + kTileKeys) / kTileKeys - from);
+        w.n = max(0, sink + max(0, min(r0 + 1, a.rows.max_len)) / kTileKeys - from - w.from);
+        return w;
+    }
+    __device__ __forceinline__ Turns touched(const WindowArgs &a, int r0, int r1) const {
+        Turns w;
+        w.low = min(sink, (max(0, min(min(a.sinks, r1 + 1), a.rows.max_len)) + kTileKeys - 1) / kTileKeys);
+        w.from = sink + max(0, max(0, r0 - a.window + 1) / kTileKeys - from);
+        w.n = max(0, sink + (max(0, min(r1 + 1, a.rows.max_len)) + kTileKeys - 1) / kTileKeys - from - w.from);
+        return w;
+    }
+};
+// With a turn before and a turn behind each run.
+__device__ __forceinline__ Turns widened(Turns w) {
+    return {w.low > 0 ? w.low + 1 : 0, w.from - 1, w.n ? w.n + 2 : 0};
+}
+
+}  // namespace
+}  // namespace stg
