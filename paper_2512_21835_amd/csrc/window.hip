@@ -863,7 +863,17 @@ hipError_t launch_tiles(const WindowArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-bool by_tiles(const WindowArgs &a) { return a.rows.max_rows * (a.n_q_heads / a.n_kv_heads) > 16; }
+// Whether a call's rows go 128 columns to a workgroup (each of which walks all keys that they see) or 16, the keys cut.
+// A workgroup of 128 takes as long for a tile of keys as a compute unit takes for 2 of 16 columns (bf16: 0.82 and
+// 0.40 us, fp32 cache and rows: 3.6 and 1.24 us); what counts are rounds of the one over the compute units, and those
+// of the other, which keep all of them busy.  64 heads of 8 groups, bf16, split and tiles: 1 sequence of 20 rows behind
+// 4096 tokens 54 and 108 us, 8 of them 184 and 116 us, 4 of 512 rows 1811 and 289 us.
+bool by_tiles(const WindowArgs &a) {
+    const long g = a.n_q_heads / a.n_kv_heads, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
+    const long small = (a.rows.rows * g / 16 + seqs) * a.n_kv_heads, large = (a.rows.rows * g / 128 + seqs) * a.n_kv_heads;
+    const long units = device_compute_units();
+    return a.rows.max_rows * g > 16 && small > 2 * units * ((large + units - 1) / units);
+}
 
 }  // namespace
 

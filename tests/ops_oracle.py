@@ -107,19 +107,17 @@ def window(b, q, out, pool, hq, window, sinks, scale=0.0):
             if not bool(see.any()):
                 o[at + t] = 0
                 continue
-            k, v = kv[see, 0], kv[see, 1]
-            for h in range(hq):
-                g = h // (hq // hkv)
-                x = q[at + t, h].double()
-                w = torch.softmax(k[:, g] @ x * scale, 0)
-                o[at + t, h] = w @ v[:, g]
-                # a score's sum of d products and its scaling, then exp's argument and its result (a few steps; the
-                # argument's rounding grows with it), all doubled as numerator and denominator may be off
-                # by as much; sums of as many probabilities as keys
-                size = float((k[:, g].abs() @ x.abs()).max()) * abs(scale)
-                term = w @ v[:, g].abs()
-                off32[at + t, h] = term * U32 * (2 * (d + 8) * size + 2 * len(k) + 32)
-                off16[at + t, h] = term * U16
+            k, v = (kv[see, x].transpose(0, 1) for x in (0, 1))     # [hkv, keys, d]
+            x = q[at + t].double().view(hkv, hq // hkv, d)
+            w = torch.softmax(x @ k.transpose(1, 2) * scale, 2)
+            o[at + t] = (w @ v).view(hq, d)
+            # a score's sum of d products and its scaling, then exp's argument and its result (a few steps; the
+            # argument's rounding grows with it), all doubled as numerator and denominator may be off
+            # by as much; sums of as many probabilities as keys
+            size = (x.abs() @ k.abs().transpose(1, 2)).amax(2).view(hq, 1) * abs(scale)
+            term = (w @ v.abs()).view(hq, d)
+            off32[at + t] = term * U32 * (2 * (d + 8) * size + 2 * k.shape[1] + 32)
+            off16[at + t] = term * U16
         at += n
     return o, off32, off16
 

@@ -170,23 +170,39 @@ def test_window_prompts(hq, hkv, d, cache, act):
         _check_window(c, _run_window(c, window, sinks), window, sinks)
 
 
+# as many KV heads as make these the calls that take whole tiles of rows at a time
+MANY_HEADS = [(50, 50, 64), (50, 50, 128), (64, 32, 128), (68, 17, 64), (72, 9, 64), (72, 9, 128)]
+
+
+@pytest.mark.parametrize("hq,hkv,d", MANY_HEADS)
 @pytest.mark.parametrize("cache", ["bf16", "fp32"])
-def test_window_long_prompt_and_long_cache(cache):
-    c = _window_case([150], [1800], 8, 1, 128, "fp32", cache)
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+def test_window_prompts_of_many_heads(hq, hkv, d, cache, act):
+    c = _window_case([37, 1, 0, 70, 2], [0, 90, 12, 45, 200], hq, hkv, d, act, cache, pad=3)
+    for window, sinks in ((0, 0), (1, 0), (20, 3), (64, 70)):
+        _check_window(c, _run_window(c, window, sinks), window, sinks)
+
+
+@pytest.mark.parametrize("hkv", [1, 8])
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+def test_window_long_prompt_and_long_cache(cache, hkv):
+    c = _window_case([150], [1800], 8 * hkv, hkv, 128, "fp32", cache)
     for window, sinks in ((300, 4), (0, 0)):
         _check_window(c, _run_window(c, window, sinks), window, sinks)
+    if hkv > 1:
+        return
     c = _window_case([1, 1], [9000, 3000], 8, 2, 128, "fp32", cache)
     for window, sinks in ((4096, 4), (0, 0), (200, 1000)):
         _check_window(c, _run_window(c, window, sinks), window, sinks)
 
 
-@pytest.mark.parametrize("rows,held", [([1, 1, 1], [3, 40, 200]), ([30, 5], [4, 100])])
+@pytest.mark.parametrize("rows,held,hkv", [([1, 1, 1], [3, 40, 200], 1), ([30, 5], [4, 100], 1), ([30, 5], [4, 100], 52)])
 @pytest.mark.parametrize("cache", ["bf16", "fp32"])
 @pytest.mark.parametrize("act", ["fp32", "bf16"])
 @pytest.mark.parametrize("d", [64, 128])
-def test_window_hides_what_is_not_finite(rows, held, cache, act, d):
+def test_window_hides_what_is_not_finite(rows, held, hkv, cache, act, d):
     """Places that a row does not see may hold anything: past the sequence, before the window, and later rows'."""
-    c = _window_case(rows, held, 4, 1, d, act, cache)
+    c = _window_case(rows, held, 4 * hkv, hkv, d, act, cache)
     b = c[0]
     used = torch.zeros(b.n_blocks, 16, dtype=torch.bool)
     for i, n in enumerate(b.lengths):
@@ -206,19 +222,21 @@ def test_window_hides_what_is_not_finite(rows, held, cache, act, d):
         b.pool[int(b.table[0, p // 16]), 1, 0, p % 16, 2] = math.nan
         got = _run_window(c, 17, 2)
         assert torch.equal(got[:n - 3], want[:n - 3]) and torch.equal(got[n:], want[n:])
-        assert bool(torch.isnan(got[n - 3:n, :, 2]).all()) and bool(torch.isinf(got[n - 3:n, :, 1::7]).all())
-        assert bool(torch.isfinite(got[n - 3:n, :, 3::7]).all())
+        assert torch.equal(got[:, 4:], want[:, 4:])
+        assert bool(torch.isnan(got[n - 3:n, :4, 2]).all()) and bool(torch.isinf(got[n - 3:n, :4, 1::7]).all())
+        assert bool(torch.isfinite(got[n - 3:n, :4, 3::7]).all())
         b.pool = clean
         b.pool[int(b.table[0, p // 16]), 0, 0, p % 16] = math.nan     # and its key
         got = _run_window(c, 17, 2)
         assert torch.equal(got[:n - 3], want[:n - 3]) and torch.equal(got[n:], want[n:])
-        assert bool(torch.isnan(got[n - 3:n]).all())
+        assert torch.equal(got[:, 4:], want[:, 4:])
+        assert bool(torch.isnan(got[n - 3:n, :4]).all())
 
 
 @pytest.mark.parametrize("act,cache", [("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "bf16")])
-@pytest.mark.parametrize("rows", [[1, 1, 1, 1], [20, 3, 40, 9]])
-def test_window_blocks_that_lead_nowhere_and_rows_that_see_nothing(rows, act, cache):
-    c = _window_case(rows, [50, 0, 33, 2], 8, 2, 64, act, cache)
+@pytest.mark.parametrize("rows,hkv", [([1, 1, 1, 1], 2), ([20, 3, 40, 9], 2), ([20, 3, 40, 9], 24)])
+def test_window_blocks_that_lead_nowhere_and_rows_that_see_nothing(rows, hkv, act, cache):
+    c = _window_case(rows, [50, 0, 33, 2], 4 * hkv, hkv, 64, act, cache)
     b = c[0]
     b.table[0, 2] = b.n_blocks
     b.table[2, 0] = -1
@@ -230,12 +248,14 @@ def test_window_blocks_that_lead_nowhere_and_rows_that_see_nothing(rows, act, ca
     assert not bool(got[rows[0]:rows[0] + rows[1]].any()) and not bool(got[b.total - rows[3]:].any())
 
 
-def test_window_scores_of_any_size():
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("hkv", [2, 76])
+def test_window_scores_of_any_size(hkv, cache):
     """Scores beyond exp's range, equal scores, and a scale of the caller's."""
     for scale, q_scale in ((0.0, 60.0), (4.0, 10.0), (1e-6, 1.0), (-0.5, 3.0)):
-        c = _window_case([1, 1, 30], [100, 3, 20], 4, 2, 64, "fp32", "bf16", scale=q_scale)
+        c = _window_case([1, 1, 30], [100, 3, 20], 2 * hkv, hkv, 64, "fp32", cache, scale=q_scale)
         _check_window(c, _run_window(c, 40, 4, scale=scale), 40, 4, scale)
-    c = _window_case([1, 9], [100, 3], 4, 2, 64, "fp32", "bf16", scale=0.0)
+    c = _window_case([1, 9], [100, 3], 2 * hkv, hkv, 64, "fp32", cache, scale=0.0)
     _check_window(c, _run_window(c, 40, 4), 40, 4)
 
 
