@@ -442,8 +442,8 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Prompts.  A workgroup: 128 CB columns = G heads x BQ = 128 CB / G consecutive rows of one sequence, one KV head; wavefront
-// w the columns 32 CB w .. (column r: head r / BQ, row r % BQ).  K and V tiles of 32 keys (two pages) go straight into
+// Prompts.  A workgroup: 128 columns = G heads x BQ = 128 / G consecutive rows of one sequence, one KV head; wavefront
+// w the columns 32 w .. (column r: head r / BQ, row r % BQ).  K and V tiles of 32 keys (two pages) go straight into
 // a ring of LDS stages, one barrier per tile.  S^T = K Q^T: lane l holds keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for
 // column l % 32, the k order of the operand P^T of O^T += V^T P^T; 32x32x16 MFMAs, q and p as TERMS bf16 terms.
 //
@@ -451,11 +451,11 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
 // tile t: the three are independent, and the vector instructions of the softmax (as long as the MFMAs with one
 // term) are laid between the MFMAs by hand.  Fragments are in registers half a turn before their MFMAs: V's are
 // read under the scores, K's of the tile behind under the values.
-template <int D, int CB>
+template <int D>
 struct TileLds {
     static constexpr int KEYS = 32, ROW = 2 * D, HALF = KEYS * ROW, BYTES = 2 * HALF, CH = ROW / 16;
     // tile t - 1 is read until the middle of turn t: its stage then takes tile t + S - 1
-    static constexpr int STAGES = CB == 1 && D == 128 ? 5 : 6;
+    static constexpr int STAGES = D == 128 ? 5 : 6;
     static constexpr int KPC = 1024 / ROW, COPIES = 8 / KPC;   // keys per copy; copies of K (and of V) per wavefront
     __device__ static int kx(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
     __device__ static int vx(int key) { return D == 128 ? (key & 3) << 2 : (key & 2) << 1; }
@@ -477,15 +477,15 @@ struct TilePlan {
     int log_g;
 };
 
-template <int D, int TERMS, int CB>
-__global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_tiles(WindowArgs a, TilePlan pl) {
-    using L = TileLds<D, CB>;
+template <int D, int TERMS>
+__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowArgs a, TilePlan pl) {
+    using L = TileLds<D>;
     constexpr int S = L::STAGES, KK = D / 16, NB = D / 32, KT = L::KEYS;
     constexpr int TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32;   // of q and out
     __shared__ __align__(1024) char lds[S * L::BYTES];
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, log_bq = (CB == 1 ? 7 : 8) - pl.log_g, bq = 1 << log_bq;
+    const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, log_bq = 7 - pl.log_g, bq = 1 << log_bq;
     RowBlock rb;
     if (!rb.find(a, blockIdx.x / hkv, log_bq)) return;
     const OpRows::Seq &seq = rb.seq;
@@ -532,38 +532,31 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         if (i < n_tiles) copy(i, i * L::BYTES);
 
     // the wavefront's columns and the rows that they have: positions w_first .. w_last
-    const int c0 = 32 * CB * wave, r0 = bq >= 32 * CB ? c0 & (bq - 1) : 0;
-    const int w_rows = min(bq >= 32 * CB ? 32 * CB : bq, rows - r0), w_first = first + r0, w_last = w_first + w_rows - 1;
-    bf16x8_t q[CB][TERMS][KK];
-    f32x16_t o[CB][NB];
-    float m[CB], l[CB];
-    int pos[CB];
-    size_t q_at[CB];
+    const int c0 = 32 * wave, r0 = bq >= 32 ? c0 & (bq - 1) : 0;
+    const int w_rows = min(bq >= 32 ? 32 : bq, rows - r0), w_first = first + r0, w_last = w_first + w_rows - 1;
+    bf16x8_t q[TERMS][KK];
+    f32x16_t o[NB];
+    const int r = c0 + col, t = r & (bq - 1);
+    const int pos = t < rows ? first + t : -1;
+    float m = -INFINITY, l = 0.f;
+    const size_t q_at = (size_t)(seq.first + t0 + min(t, rows - 1)) * a.q_ld + (size_t)((g << pl.log_g) + (r >> log_bq)) * D + 8 * half;
 #pragma unroll
-    for (int x = 0; x < CB; ++x) {
-        const int r = c0 + 32 * x + col, t = r & (bq - 1);
-        pos[x] = t < rows ? first + t : -1;
-        m[x] = -INFINITY;
-        l[x] = 0.f;
-        q_at[x] = (size_t)(seq.first + t0 + min(t, rows - 1)) * a.q_ld + (size_t)((g << pl.log_g) + (r >> log_bq)) * D + 8 * half;
+    for (int kk = 0; kk < KK; ++kk) {
+        float v[8];
+        load4(a.q, q_at + 16 * kk, TYPE, v);
+        load4(a.q, q_at + 16 * kk + 4, TYPE, v + 4);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            float v[8];
-            load4(a.q, q_at[x] + 16 * kk, TYPE, v);
-            load4(a.q, q_at[x] + 16 * kk + 4, TYPE, v + 4);
+        for (int j = 0; j < 8; ++j) {
+            __bf16 s[TERMS];
+            split_terms<TERMS>(a.scale < 0.f ? -v[j] : v[j], s);   // (its scores' maximum is then the largest)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                __bf16 s[TERMS];
-                split_terms<TERMS>(a.scale < 0.f ? -v[j] : v[j], s);   // (its scores' maximum is then the largest)
-#pragma unroll
-                for (int i = 0; i < TERMS; ++i) q[x][i][kk][j] = s[i];
-            }
+            for (int i = 0; i < TERMS; ++i) q[i][kk][j] = s[i];
         }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[x][b][i] = 0.f;
     }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
     bool odd = false;
     const float scale = fabsf(a.scale) * kLog2e;   // scores in base 2
     const uint32_t k_at = ring + col * L::ROW + 16 * (half ^ L::kx(col));   // chunk 2 kk + half of key col, permuted
@@ -591,13 +584,12 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
         }
     };
-    auto hide = [&](f32x16_t(&s)[CB], int t) {
+    auto hide = [&](f32x16_t &s, int t) {
         const int k0 = rb.tile_at(t) * KT + 4 * half;   // the lane's first key; its others are 8 (i / 4) + i % 4 further
         uint32_t pages = t < n_tiles ? ~0u : 0u;
         if (strange && t < n_tiles)
             pages = (known(seq.table[rb.page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[rb.page_at(t, 1)]) ? 0xFFFF0000u : 0u);
-#pragma unroll
-        for (int x = 0; x < CB; ++x) hide_scores(s[x], pages >> (4 * half) & seen_bits(a, pos[x], k0));
+        hide_scores(s, pages >> (4 * half) & seen_bits(a, pos, k0));
     };
     auto value_frag = [&](uint32_t v, int h, int b) {
         const uint32_t at = (v ^ (64 * b)) + 16 * h * L::ROW;
@@ -608,38 +600,33 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     // The maximum that scores are taken relative to: a whole number (so that rescaling is exact, what is already
     // rounded to bf16 included) which stays until a score is 2^kSlack beyond it: p and its sums are floating
     // point, and the rescaling, a quarter of a tile's vector work, is rare after the first tile.
-    auto raise = [&](const float(&top)[CB], bf16x8_t(&p)[CB][TERMS][2]) {
+    auto raise = [&](float top, bf16x8_t(&p)[TERMS][2]) {
+        const float best = fmaxf(top, lane_xor(top, 32)) * scale;
+        if (__builtin_amdgcn_ballot_w64(best > m + kSlack) == 0) return;
+        const float to = best > m + kSlack ? ceilf(best) : m;
+        const float alpha = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
+        m = to;
+        l *= alpha;
 #pragma unroll
-        for (int x = 0; x < CB; ++x) {
-            const float best = fmaxf(top[x], lane_xor(top[x], 32)) * scale;
-            if (__builtin_amdgcn_ballot_w64(best > m[x] + kSlack) == 0) continue;
-            const float to = best > m[x] + kSlack ? ceilf(best) : m[x];
-            const float alpha = __builtin_amdgcn_exp2f(m[x] - (to == -INFINITY ? 0.f : to));
-            m[x] = to;
-            l[x] *= alpha;
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[x][b][i] *= alpha;
-#pragma unroll
-            for (int i = 0; i < TERMS; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) p[x][i][h][j] = (__bf16)((float)p[x][i][h][j] * alpha);
-        }
-    };
-
-    f32x16_t s[CB];               // scores of tile t
-    bf16x8_t p[CB][TERMS][2];     // probabilities of tile t - 1
-#pragma unroll
-    for (int x = 0; x < CB; ++x)
+            for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
 #pragma unroll
         for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) p[x][i][h] = bf16x8_t{};
-    constexpr int N1 = CB * TERMS * KK, N2 = CB * TERMS * 2 * NB;   // MFMAs of the scores, of the values
-    constexpr int EXPS = 8 * CB, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[i][h][j] = (__bf16)((float)p[i][h][j] * alpha);
+    };
+
+    f32x16_t s;               // scores of tile t
+    bf16x8_t p[TERMS][2];     // probabilities of tile t - 1
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) p[i][h] = bf16x8_t{};
+    constexpr int N1 = TERMS * KK, N2 = TERMS * 2 * NB;   // MFMAs of the scores, of the values
+    constexpr int EXPS = 8, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
 
     bf16x8_t kf[KK];   // of tile t + 1
     auto load_key = [&](uint32_t at, int kk) { kf[kk] = __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + at) ^ (32 * kk))); };
@@ -654,25 +641,17 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     lds_barrier();
     load_keys(0);
 #pragma unroll
-    for (int x = 0; x < CB; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-        for (int x = 0; x < CB; ++x)
-#pragma unroll
-            for (int i = 0; i < TERMS; ++i) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], q[x][i][kk], s[x], 0, 0, 0);
+        for (int i = 0; i < TERMS; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], q[i][kk], s, 0, 0, 0);
     load_keys(L::BYTES);
     hide(s, 0);
     {
-        float top[CB];
+        float top = s[0];
 #pragma unroll
-        for (int x = 0; x < CB; ++x) {
-            top[x] = s[x][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top[x] = fmaxf(top[x], s[x][i]);
-        }
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         raise(top, p);
     }
     uint32_t at_new = (S - 1) * L::BYTES, at_keys = 2 * L::BYTES, at_values = 0;   // stages of tiles t + S - 1, t + 2, t - 1
@@ -701,34 +680,29 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             }
             continue;
         }
-        f32x16_t n[CB];
-        bf16x8_t pn[CB][TERMS][2], vf[2 * NB];
-        float ref[CB], sum[CB];
+        f32x16_t n;
+        bf16x8_t pn[TERMS][2], vf[2 * NB];
+        const float ref = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
 #pragma unroll
-        for (int x = 0; x < CB; ++x) {
-            ref[x] = m[x] == -INFINITY ? 0.f : m[x];
-            sum[x] = 0.f;
+        for (int i = 0; i < 16; ++i) n[i] = 0.f;
+        auto softmax_piece = [&](int e) {   // scores 2 e and the one behind it
 #pragma unroll
-            for (int i = 0; i < 16; ++i) n[x][i] = 0.f;
-        }
-        auto softmax_piece = [&](int e) {   // scores 2 (e % 8) and the one behind it of block e / 8
-            const int x = e / 8;
-#pragma unroll
-            for (int i = 2 * (e % 8); i < 2 * (e % 8) + 2; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[x][i], scale, -ref[x]));
-                sum[x] += w;
+            for (int i = 2 * e; i < 2 * e + 2; ++i) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
+                sum += w;
                 __bf16 b[TERMS];
                 split_terms<TERMS>(w, b);
 #pragma unroll
-                for (int j = 0; j < TERMS; ++j) pn[x][j][i / 8][i % 8] = b[j];
+                for (int j = 0; j < TERMS; ++j) pn[j][i / 8][i % 8] = b[j];
             }
-            asm volatile("" : "+v"(sum[x]));   // (here, and not where the sums are needed)
+            asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)
         };
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < N1; ++c) {
-            const int kk = c / (CB * TERMS), x = c % (CB * TERMS) / TERMS, i = c % TERMS;
-            n[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], q[x][i][kk], n[x], 0, 0, 0);
+            const int kk = c / TERMS, i = c % TERMS;
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], q[i][kk], n, 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int f = 0; f < 2 * NB; ++f)
@@ -745,12 +719,12 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
         middle(t);
         const bool more = t + S - 1 < n_tiles;
         if (!my_clear.has(t + 1) | strange) hide(n, t + 1);
-        float top[CB];
+        float top;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < N2; ++c) {
-            const int f = c / (CB * TERMS), x = c % (CB * TERMS) / TERMS, i = c % TERMS;   // fragment (h, b) = (f / NB, f % NB)
-            o[x][f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], p[x][i][f / NB], o[x][f % NB], 0, 0, 0);
+            const int f = c / TERMS, i = c % TERMS;   // fragment (h, b) = (f / NB, f % NB)
+            o[f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], p[i][f / NB], o[f % NB], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int e = 0; e < 2 * L::COPIES; ++e)
@@ -764,21 +738,18 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
 #pragma unroll
             for (int e = 0; e < EXPS; ++e)
                 if (e * N2 / EXPS == c) {
-                    const float u = n[e / 8][2 * (e % 8)], v = n[e / 8][2 * (e % 8) + 1];
-                    if (e % 8 == 0) top[e / 8] = fmaxf(u, v);
-                    else asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top[e / 8]) : "v"(u), "v"(v));   // (fmaxf quiets each operand first)
+                    const float u = n[2 * e], v = n[2 * e + 1];
+                    if (e == 0) top = fmaxf(u, v);
+                    else asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top) : "v"(u), "v"(v));   // (fmaxf quiets each operand first)
                 }
             __builtin_amdgcn_sched_barrier(0);
         }
+        l += sum;
+        s = n;
 #pragma unroll
-        for (int x = 0; x < CB; ++x) {
-            l[x] += sum[x];
-            s[x] = n[x];
+        for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-            for (int i = 0; i < TERMS; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) p[x][i][h] = pn[x][i][h];
-        }
+            for (int h = 0; h < 2; ++h) p[i][h] = pn[i][h];
         raise(top, p);
     }
     // whether any wavefront cleared a V
@@ -796,34 +767,31 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
             const int b = ((const_ints)(uintptr_t)seq.table)[page];
             if (!known(b) || (clear.has(t) && !strange)) continue;
             const size_t place = (size_t)b * block_bytes + at % kPage * L::ROW;
+            float w = 0.f;
 #pragma unroll
-            for (int x = 0; x < CB; ++x) {
-                float w = 0.f;
+            for (int kk = 0; kk < KK; ++kk) {
+                const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(gk + place + 32 * kk);
+                float v[8];
+                load4(a.q, q_at + 16 * kk, TYPE, v);
+                load4(a.q, q_at + 16 * kk + 4, TYPE, v + 4);
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(gk + place + 32 * kk);
-                    float v[8];
-                    load4(a.q, q_at[x] + 16 * kk, TYPE, v);
-                    load4(a.q, q_at[x] + 16 * kk + 4, TYPE, v + 4);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w = fmaf(v[j], (float)k[j], w);
-                    asm volatile("" ::: "memory");   // (registers)
-                }
-                w += lane_xor(w, 32);
-                w = __builtin_amdgcn_exp2f(fmaf(w, a.scale * kLog2e, m[x] == -INFINITY ? 0.f : -m[x]));
-                if (!sees(a, pos[x], at)) continue;
-#pragma unroll
-                for (int c = 0; c < NB; ++c)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float v[4];
-                        load4(gv + place, 32 * c + 8 * j, STAGE_BF16, v);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            o[x][c][4 * j + i] = fabsf(v[i]) < INFINITY ? o[x][c][4 * j + i] : fmaf(w, v[i], o[x][c][4 * j + i]);
-                        __builtin_amdgcn_sched_barrier(0);   // (registers)
-                    }
+                for (int j = 0; j < 8; ++j) w = fmaf(v[j], (float)k[j], w);
+                asm volatile("" ::: "memory");   // (registers)
             }
+            w += lane_xor(w, 32);
+            w = __builtin_amdgcn_exp2f(fmaf(w, a.scale * kLog2e, m == -INFINITY ? 0.f : -m));
+            if (!sees(a, pos, at)) continue;
+#pragma unroll
+            for (int c = 0; c < NB; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float v[4];
+                    load4(gv + place, 32 * c + 8 * j, STAGE_BF16, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        o[c][4 * j + i] = fabsf(v[i]) < INFINITY ? o[c][4 * j + i] : fmaf(w, v[i], o[c][4 * j + i]);
+                    __builtin_amdgcn_sched_barrier(0);   // (registers)
+                }
         }
     }
     // Rows are stored 16 bytes a lane, neighbouring lanes side by side, by way of the ring (8 bytes a lane, each row's
@@ -831,35 +799,32 @@ __global__ __launch_bounds__(256, CB == 1 && TERMS == 1 ? 2 : 1) void window_til
     constexpr int E = TYPE == STAGE_F32 ? 4 : 2, OROW = D * E + 16, OCH = D * E / 16;
     static_assert(64 + 4 * 32 * OROW <= S * L::BYTES, "the ring holds the output rows");
     char *const out_lds = lds + 64 + wave * 32 * OROW;   // (behind the flags)
+    const float sum = l + lane_xor(l, 32);
 #pragma unroll
-    for (int x = 0; x < CB; ++x) {
-        const float sum = l[x] + lane_xor(l[x], 32);
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int j = 0; j < 4; ++j)
+            store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, TYPE,
+                   quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, TYPE,
-                       quotient(make_float4(o[x][b][4 * j], o[x][b][4 * j + 1], o[x][b][4 * j + 2], o[x][b][4 * j + 3]), sum));
-#pragma unroll
-        for (int i = 0; i < 32 * OCH / 64; ++i) {
-            const int e = 64 * i + lane, r = c0 + 32 * x + e / OCH, t = r & (bq - 1);
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(out_lds + e / OCH * OROW + e % OCH * 16);
-            if (t < rows)
-                *reinterpret_cast<u32x4 *>(static_cast<char *>(a.out) + E * ((size_t)(seq.first + t0 + t) * a.out_ld +
-                                           (size_t)((g << pl.log_g) + (r >> log_bq)) * D) + e % OCH * 16) = v;
-        }
+    for (int i = 0; i < 32 * OCH / 64; ++i) {
+        const int e = 64 * i + lane, r = c0 + e / OCH, t = r & (bq - 1);
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(out_lds + e / OCH * OROW + e % OCH * 16);
+        if (t < rows)
+            *reinterpret_cast<u32x4 *>(static_cast<char *>(a.out) + E * ((size_t)(seq.first + t0 + t) * a.out_ld +
+                                       (size_t)((g << pl.log_g) + (r >> log_bq)) * D) + e % OCH * 16) = v;
     }
 }
 
-template <int D, int TERMS, int CB>
+template <int D, int TERMS>
 hipError_t launch_tiles(const WindowArgs &a, hipStream_t st) {
     TilePlan p{};
     while (a.n_kv_heads << p.log_g < a.n_q_heads) ++p.log_g;
     // row blocks: no sequence adds more than one that is not full
-    const int bq = 128 * CB >> p.log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
+    const int bq = 128 >> p.log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
     const long blocks = ((long)a.rows.rows / bq + seqs) * a.n_kv_heads;
     if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-    STG_LAUNCH((window_tiles<D, TERMS, CB>), dim3((unsigned)blocks), dim3(256), 0, st, a, p);
+    STG_LAUNCH((window_tiles<D, TERMS>), dim3((unsigned)blocks), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }
 
@@ -889,7 +854,7 @@ hipError_t launch_window_attention(const WindowArgs &a, hipStream_t st) {
     if (f32 && by_tiles(a)) return launch_window_f32(a, st);
 #define STG_WINDOW_CASE(D)                                                 \
     if (a.head_dim == D && by_tiles(a))                                    \
-        return exact ? launch_tiles<D, 3, 1>(a, st) : launch_tiles<D, 1, 1>(a, st); \
+        return exact ? launch_tiles<D, 3>(a, st) : launch_tiles<D, 1>(a, st); \
     if (a.head_dim == D)                                                   \
         return f32 ? launch_split<D, true, 1>(a, st)                       \
                    : exact ? launch_split<D, false, 3>(a, st) : launch_split<D, false, 1>(a, st);
