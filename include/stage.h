@@ -155,13 +155,26 @@ typedef struct {
        next load number, so that they fail: a self-test of the detection path that changes no
        weight and no output. */
     int32_t slot_check;
+    /* What a layer's attention block has beyond the plain one (all 0: nothing, and the calls are the same as
+       without these fields).  With any of them head_dim must be 64 or 128 and n_q_heads / n_kv_heads 1, 2, 4 or 8.
+       head_norm 1: query and key heads are normalised before their rotation, x / sqrt(mean(x^2) + rms_eps) * gain,
+       by gains of head_dim elements that all query and all key heads share (stage_layer_weights.gq, gk).
+       window > 0: a token attends to the last `window` tokens (itself included) and to the sequence's first `sinks`;
+       the cache keeps them all.  sinks needs a window.
+       max_adapters > 0: up to that many low-rank adapters (stage_load_adapter, stage_set_adapter), of rank up to
+       adapter_rank, a multiple of 4 of at most STAGE_OPS_MAX_RANK (include/stage_ops.h). */
+    int32_t head_norm;
+    int32_t window, sinks;
+    int32_t max_adapters, adapter_rank;
 } stage_config;
 
 /* Weights of one decoder layer: bf16 bit patterns, host or device memory, read only during
    the call.  wq [Hq*d, H], wk [Hkv*d, H], wv [Hkv*d, H], wo [H, Hq*d], wg [F, H], wu [F, H],
-   wd [H, F], g1 [H] (attention RMSNorm gain), g2 [H] (MLP RMSNorm gain). */
+   wd [H, F], g1 [H] (attention RMSNorm gain), g2 [H] (MLP RMSNorm gain).  gq, gk [d] (gains of the
+   query and key heads): read with stage_config.head_norm only; they belong to the MHA block. */
 typedef struct {
     const void *wq, *wk, *wv, *wo, *wg, *wu, *wd, *g1, *g2;
+    const void *gq, *gk;
 } stage_layer_weights;
 
 /* Fills *cfg with defaults: theta 10000, eps 1e-5, kv_block_tokens 16, n_stream_slots 2,
@@ -186,6 +199,26 @@ int stage_destroy(stage *s);
    III-E).  EINVAL: bad layer or code; ENOMEM: the resident blocks would exceed the weight budget,
    or allocation failed (the layer is unchanged); ESTATE: w == NULL for a layer never loaded. */
 int stage_load_layer(stage *s, int32_t layer, const stage_layer_weights *w, int32_t resident);
+
+/* Low-rank adapters of sequences beside the shared projections (stage_config.max_adapters): the output of projection
+   `target` becomes W x + scale B (A x) for the rows of sequences with adapter `id`.  Targets: the QKV projection
+   (x: the normalised input, [n_q_heads + 2 n_kv_heads] d outputs, q heads, k heads, v heads; adapters of one of them
+   alone have zero rows of B elsewhere, those of several are stacked), the O projection and the down projection. */
+#define STAGE_ADAPT_QKV 0
+#define STAGE_ADAPT_O 1
+#define STAGE_ADAPT_DOWN 2
+
+/* Sets adapter `id` (0 <= id < max_adapters) of a layer's projection: a [rank, in], b [out, rank] (bf16 bit patterns,
+   host or device memory, read only during the call).  rank 0 takes it out (a and b are not read); a sequence's
+   adapter adds nothing where none is set.  The weights stay in HBM, max_adapters * adapter_rank * (in + out) elements
+   from the first adapter of a layer's projection on; they count towards no budget.  Waits for the stage's
+   streams.  EINVAL: bad ids, rank above adapter_rank, a scale that is not finite; ENOMEM. */
+int stage_load_adapter(stage *s, int32_t layer, int32_t target, int32_t id, int32_t rank, float scale,
+                       const void *a, const void *b);
+
+/* The adapter of sequence (mb, b) in later calls: 0 <= id < max_adapters, or -1 for none (as at first and after
+   stage_reset_sequence). */
+int stage_set_adapter(stage *s, int32_t mb, int32_t b, int32_t id);
 
 /* Prefill: runs T new tokens of each of B rows of each listed micro-batch through all layers.
    x_in, x_out: device fp32 [n_mb][B][T][hidden] (x_out may not alias x_in).  Row r of x_out is
@@ -239,7 +272,8 @@ int stage_prefill_lane(stage *s, int32_t lane, int32_t n_mb, const int32_t *mb_i
    lanes) race; calls ordered on one stream are safe.  The caller still owns x_in and x_out.
    ENOMEM: the call needs more scratch than the array holds (the message gives the bytes; it
    grows with rows x (2 Hq d + ffn) and rows x Hq x ceil(context / 64) x (d + 2), plus a split-K
-   area for 3 rows or more); ESTATE: the call would allocate -- a residency change is due (the
+   area for 3 rows or more; with head_norm, window or adapters also with rows x (Hq + 2 Hkv) d, rows x 2 ffn and
+   the states of the keys' ranges); ESTATE: the call would allocate -- a residency change is due (the
    threshold schedule or the planner), stream slots have not been allocated yet (run one
    stage_decode first), or a sequence of the call has a parked KV tail; otherwise as
    stage_decode.  Nothing changes on an error. */

@@ -11,6 +11,7 @@ from .stage import (  # noqa: F401
     STAGE_MAX_CONTEXT, STAGE_MAX_LANES, stage_decode_lane, stage_prefill_lane, stage_decode_noalloc,
     STAGE_NOALLOC_SCRATCH_BYTES,
     STAGE_RES_OFFLOADED, STAGE_RES_RESIDENT, STAGE_RES_MHA_OFFLOADED, STAGE_RES_MLP_OFFLOADED,
+    STAGE_ADAPT_QKV, STAGE_ADAPT_O, STAGE_ADAPT_DOWN, stage_load_adapter, stage_set_adapter,
     stage_config_default, stage_init, stage_destroy, stage_load_layer, stage_prefill, stage_decode,
     stage_kv_append, stage_kv_export_tail, stage_reset_sequence, stage_sync, stage_get_block_table,
     stage_kv_park, stage_kv_unpark,

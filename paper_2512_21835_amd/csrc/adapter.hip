@@ -51,6 +51,13 @@ __device__ __forceinline__ void store8(void *p, size_t e, int type, const float 
         *reinterpret_cast<bf16x8_t *>(static_cast<uint16_t *>(p) + e) = b;
     }
 }
+// Eight elements of a hi/lo pair, whose sum is exact.
+__device__ __forceinline__ void load8_pair(const void *p, size_t at, float v[8]) {
+    const uint16_t *const h = static_cast<const uint16_t *>(p) + at;
+    const bf16x8_t hi = *reinterpret_cast<const bf16x8_t *>(h), lo = *reinterpret_cast<const bf16x8_t *>(h + 32);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)hi[j] + (float)lo[j];
+}
 // x as a sum of bf16 terms, each the nearest to what the ones before leave: three terms hold all 24 bits.
 template <int TERMS>
 __device__ __forceinline__ void split_terms8(const float v[8], bf16x8_t t[TERMS]) {
@@ -108,7 +115,10 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, Adapte
         const int e = 64 * i + lane, r = e / CH, k = k0 + e % CH * 8;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-        if (k < k1 && row0 + r < a.rows) load8(a.x, (size_t)(row0 + r) * a.x_ld + k, TYPE, v[i]);
+        if (k < k1 && row0 + r < a.rows) {
+            if (TYPE == STAGE_F32 && a.x_pair) load8_pair(a.x, (size_t)(row0 + r) * a.x_ld + pair_at(k), v[i]);
+            else load8(a.x, (size_t)(row0 + r) * a.x_ld + k, TYPE, v[i]);
+        }
     }
     TileIds t;
     t.load(a, row0);
@@ -536,6 +546,11 @@ hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles,
     return shared ? launch(Four{}, Most{}) : launch(One{}, Most{});
 }
 
+__global__ __launch_bounds__(256) void adapter_rows_kernel(SeqAdapters of, int rows, int rows_per_seq, int *ids) {
+    const int row = blockIdx.x * 256 + threadIdx.x;
+    if (row < rows) ids[row] = of.id[row / rows_per_seq];
+}
+
 }  // namespace
 
 size_t adapter_workspace(const AdapterArgs &a) {
@@ -555,6 +570,12 @@ hipError_t launch_adapter_add(const AdapterArgs &a, hipStream_t st) {
         STG_LAUNCH(adapter_down_kernel<1>, down, dim3(256), 0, st, a, p);
         return launch_up<STAGE_BF16>(a, p, tiles, st);
     }
+}
+
+hipError_t launch_adapter_rows(const SeqAdapters &of, int rows, int rows_per_seq, int *ids, hipStream_t st) {
+    if (rows <= 0) return hipSuccess;
+    STG_LAUNCH(adapter_rows_kernel, dim3((rows + 255) / 256), dim3(256), 0, st, of, rows, rows_per_seq, ids);
+    return hipGetLastError();
 }
 
 }  // namespace stg

@@ -89,7 +89,7 @@ __device__ __forceinline__ uint16_t to_bf16(float f) {
 
 template <int MODE> struct Shape {
     static constexpr bool kNorm = MODE != GEMV_PLAIN_RESIDUAL;
-    static constexpr int NW = MODE == GEMV_PLAIN_RESIDUAL ? 1 : 2;  // weight rows per unit
+    static constexpr int NW = MODE == GEMV_PLAIN_RESIDUAL || MODE == GEMV_NORM_STORE ? 1 : 2;  // weight rows per unit
 };
 
 template <int MODE>
@@ -162,6 +162,8 @@ __device__ __forceinline__ void epi_store(const GemvArgs &a, const EpiIn &e, int
         a.out[m * a.out_ld + u] = e.res + y0;
     } else if (MODE == GEMV_NORM_SWIGLU) {
         a.out[m * a.out_ld + u] = y0 / (1.f + expf(-y0)) * y1;
+    } else if (MODE == GEMV_NORM_STORE) {
+        a.out[m * a.out_ld + u] = y0;
     } else {
         const int d = a.kv.head_dim, half = d / 2;
         const int h = u / half, i = u % half;
@@ -567,7 +569,7 @@ void launch_one(const GemvArgs &c, hipStream_t st, hipEvent_t e0, hipEvent_t e1)
 template <int M, int MODE>
 void launch_rows(const GemvArgs &c, hipStream_t st, hipEvent_t e0, hipEvent_t e1) {
     const long work = (long)host_units(MODE, c) * c.K;
-    if (MODE == GEMV_PLAIN_RESIDUAL) {
+    if (Shape<MODE>::NW == 1) {
         if (M == 1 && (c.K >= 2 * c.N || work >= 60L * 1000 * 1000)) launch_one<M, 8, 1, MODE>(c, st, e0, e1);
         else if (M == 1) launch_one<M, 4, 2, MODE>(c, st, e0, e1);
         else if (M == 2 && work >= 200L * 1000 * 1000) launch_one<M, 8, 1, MODE>(c, st, e0, e1);
@@ -657,6 +659,7 @@ hipError_t launch_gemv(int mode, GemvArgs a, hipStream_t st, hipEvent_t ev_start
         case GEMV_PLAIN_RESIDUAL: return launch_mode<GEMV_PLAIN_RESIDUAL>(a, st, ev_start, ev_stop);
         case GEMV_NORM_SWIGLU: return launch_mode<GEMV_NORM_SWIGLU>(a, st, ev_start, ev_stop);
         case GEMV_NORM_ROPE_KV: return launch_mode<GEMV_NORM_ROPE_KV>(a, st, ev_start, ev_stop);
+        case GEMV_NORM_STORE: return launch_mode<GEMV_NORM_STORE>(a, st, ev_start, ev_stop);
         default: return hipErrorInvalidValue;
     }
 }

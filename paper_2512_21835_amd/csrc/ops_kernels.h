@@ -80,6 +80,7 @@ struct WindowArgs {
     int window, sinks;         // window > 0
     float scale;
     float *part;               // workspace: states of rows whose keys are cut
+    int pair_rows;             // (fp32) rows of `out` below it become the hi/lo pair of a GEMM operand, in the row's own bytes
     OpRows rows;
 };
 // Bytes of WindowArgs::part that a call takes (it looks at the sizes only).
@@ -91,6 +92,7 @@ struct AdapterArgs {
     const void *x, *base;
     void *out;
     int type;
+    int x_pair;                // x: the hi/lo pair of a GEMM operand (x_ld: of the pair)
     long x_ld, base_ld, out_ld;
     int rows, k, n, n_adapters, max_rank;
     const uint16_t *a, *b;
@@ -100,5 +102,10 @@ struct AdapterArgs {
 };
 size_t adapter_workspace(const AdapterArgs &a);
 hipError_t launch_adapter_add(const AdapterArgs &a, hipStream_t st);
+// ids[row] = of.id[row / rows_per_seq]
+struct SeqAdapters {
+    int id[kMaxSeqs];
+};
+hipError_t launch_adapter_rows(const SeqAdapters &of, int rows, int rows_per_seq, int *ids, hipStream_t st);
 
 }  // namespace stg

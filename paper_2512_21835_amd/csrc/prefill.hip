@@ -727,20 +727,24 @@ hipError_t launch_gemm(int mode, const GemmArgs &a, int n_mats, hipStream_t st) 
     return hipGetLastError();
 }
 
+hipError_t launch_qkv_product(const GemmArgs &g, float **qkv, int *n_part, hipStream_t st) {
+    *n_part = 1;
+    *qkv = g.out;
+    if (g.K % BK != 0) return launch_gemm(GEMM_STORE, g, 1, st);
+    if (g.lda < pair_ld(g.K)) return hipErrorInvalidValue;
+    const GemmPlan p = gemm_plan(g.M, g.N, g.K, false, g.part != nullptr, g.part_cap64);
+    *n_part = p.parts();
+    if (*n_part > 1) *qkv = g.part;
+    launch_plan<GEMM_STORE>(g, p, st);
+    return hipGetLastError();
+}
+
 hipError_t launch_qkv(const GemmArgs &g, RopeKvArgs r, hipStream_t st) {
     if (g.M <= 0) return hipSuccess;
-    r.n_part = 1;
-    r.qkv = g.out;
-    if (g.K % BK != 0) {
-        const hipError_t e = launch_gemm(GEMM_STORE, g, 1, st);
-        if (e != hipSuccess) return e;
-    } else {
-        if (g.lda < pair_ld(g.K)) return hipErrorInvalidValue;
-        const GemmPlan p = gemm_plan(g.M, g.N, g.K, false, g.part != nullptr, g.part_cap64);
-        r.n_part = p.parts();
-        if (r.n_part > 1) r.qkv = g.part;
-        launch_plan<GEMM_STORE>(g, p, st);
-    }
+    float *qkv = nullptr;
+    const hipError_t e = launch_qkv_product(g, &qkv, &r.n_part, st);
+    if (e != hipSuccess) return e;
+    r.qkv = qkv;
     return launch_rope_kv_store(r, st);
 }
 

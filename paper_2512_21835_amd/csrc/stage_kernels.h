@@ -57,7 +57,8 @@ struct KvView {
 enum GemvMode {
     GEMV_PLAIN_RESIDUAL = 1, // out = res + W act
     GEMV_NORM_SWIGLU = 2,    // out = silu(Wg y) * (Wu y), y = rmsnorm(act) * gain
-    GEMV_NORM_ROPE_KV = 3    // [q | k | v] = Wqkv y; rotate q, k; q -> q_out, k and v -> KV cache
+    GEMV_NORM_ROPE_KV = 3,   // [q | k | v] = Wqkv y; rotate q, k; q -> q_out, k and v -> KV cache
+    GEMV_NORM_STORE = 4      // out = W y (what follows the QKV projection has launches of its own)
 };
 
 struct GemvArgs {
@@ -160,8 +161,9 @@ struct RopeKvArgs {
     RowMap meta;
 };
 hipError_t launch_rope_kv_store(const RopeKvArgs &a, hipStream_t st);
-// The QKV projection and what follows it (r.qkv and r.n_part are set here): g.out is where an uncut
-// product goes.
+// The QKV projection: its product, as the sum of *n_part parts of M x N at *qkv (the uncut one goes to g.out).
+hipError_t launch_qkv_product(const GemmArgs &g, float **qkv, int *n_part, hipStream_t st);
+// The QKV projection and what follows it (r.qkv and r.n_part are set here).
 hipError_t launch_qkv(const GemmArgs &g, RopeKvArgs r, hipStream_t st);
 
 struct AttnArgs {

@@ -36,8 +36,10 @@
 #include <vector>
 
 #include "device_guard.h"
+#include "ops_kernels.h"
 #include "stage.h"
 #include "stage_kernels.h"
+#include "stage_ops.h"
 
 using namespace stg;
 
@@ -49,6 +51,7 @@ namespace {
 
 constexpr int kDecodeSplitKeys = 64;
 constexpr int kMaxContext = 16384;  // decode attention merges at most 256 splits of 64 keys
+constexpr int kMaxAdapters = 65536;
 constexpr int kTimeAll = STAGE_TIME_CALLS | STAGE_TIME_GATEUP | STAGE_TIME_LAYERS;
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -62,9 +65,19 @@ struct Block {
     void *host_dev = nullptr;  // the pinned copy as kernels address it (zero copy)
 };
 
+// The adapters of a layer's projection, in HBM from the first one on.
+struct Adapters {
+    uint16_t *a = nullptr, *b = nullptr;   // [max_adapters][adapter_rank][in], [max_adapters][out][adapter_rank]
+    int *ranks = nullptr;
+    float *scales = nullptr;
+    std::vector<int> set;                  // the ranks, as the host knows them
+    int n_set = 0;                         // of rank 1 or more
+};
+
 struct Layer {
     bool loaded = false;
     Block blk[2];
+    Adapters adapters[3];      // by STAGE_ADAPT_*
     // any block offloaded: the layer takes a slot load in every staged call
     bool streams() const { return loaded && !(blk[kMha].resident && blk[kMlp].resident); }
 };
@@ -111,6 +124,8 @@ struct LaneState {
     float *ws_part_o = nullptr, *ws_part_ml = nullptr;
     float *ws_split = nullptr, *ws_split_ss = nullptr;
     size_t split_floats = 0;
+    void *ws_ops = nullptr;
+    size_t ops_bytes = 0;
 };
 
 struct stage {
@@ -122,6 +137,7 @@ struct stage {
 
     // offsets inside the MHA block (wqkv, wo, g1) and inside the MLP block (wg, wu, wd, g2)
     size_t off_wqkv = 0, off_wo = 0, off_wg = 0, off_wu = 0, off_wd = 0, off_g1 = 0, off_g2 = 0;
+    size_t off_gq = 0, off_gk = 0;   // (head_norm; in the MHA block)
     size_t blk_bytes[2] = {0, 0};
     size_t blob_bytes = 0;  // one layer: both blocks
     std::vector<Layer> layers;
@@ -155,6 +171,10 @@ struct stage {
     float *ws_part_o = nullptr, *ws_part_ml = nullptr;
     float *ws_split = nullptr, *ws_split_ss = nullptr;  // partial products of projections cut in K
     size_t split_floats = 0;                            // of ws_split
+    void *ws_ops = nullptr;   // a call's adapter per row, then the window's states or the adapters' sums (ops_layout)
+    size_t ops_bytes = 0;
+    int max_ctx = 0;          // longest sequence of the call in flight
+    std::vector<int> adapter_of;   // per sequence (-1: none)
     void *ws_dense = nullptr;
     size_t ws_dense_bytes = 0;
 
@@ -267,6 +287,8 @@ void swap_workspaces(stage *s, LaneState &o) {
     std::swap(s->ws_split, o.ws_split);
     std::swap(s->ws_split_ss, o.ws_split_ss);
     std::swap(s->split_floats, o.split_floats);
+    std::swap(s->ws_ops, o.ws_ops);
+    std::swap(s->ops_bytes, o.ops_bytes);
 }
 
 // Exchanges the stage's call state (lane 0's, or the lane swapped in) with lanes[l]'s.
@@ -359,6 +381,12 @@ size_t resident_bytes(const stage *s) {
 
 // The weight budget: n_resident_max whole layers' worth of HBM, spent block by block.
 size_t budget_bytes(const stage *s) { return (size_t)s->cfg.n_resident_max * s->blob_bytes; }
+
+void free_adapters(Adapters &d) {
+    for (void *p : {(void *)d.a, (void *)d.b, (void *)d.ranks, (void *)d.scales})
+        if (p) (void)hipFree(p);
+    d = Adapters();
+}
 
 void free_block(Block &k) {
     if (k.dev) (void)hipFree(k.dev);
@@ -500,6 +528,15 @@ size_t part_floats(const stage *s, size_t rows) {
     return n;
 }
 
+// Floats per row of ws_qkv, elements per row of ws_pair.  ws_qkv holds the prefill QKV rows, the pair of h, or
+// (widths off 32) the gate and up halves side by side.
+size_t wide_floats(const stage *s) {
+    return std::max<size_t>(std::max<size_t>(s->qkv_rows, s->H % 32 ? 2 * (size_t)s->F : 0), (size_t)pair_ld(s->F) / 2);
+}
+size_t pair_elems(const stage *s) {
+    return (size_t)pair_ld(std::max<size_t>(std::max<size_t>(s->H, (size_t)s->Hq * s->D), s->F));
+}
+
 // need_part: rows of attention partials, max_splits states each.
 int ensure_workspace(stage *s, size_t rows, size_t need_part) {
     if (rows <= s->ws_rows && need_part <= s->part_rows) return STAGE_OK;
@@ -512,12 +549,9 @@ int ensure_workspace(stage *s, size_t rows, size_t need_part) {
         s->ws_pair = nullptr;
         s->ws_rows = 0;
         const size_t qd = (size_t)s->Hq * s->D;
-        // ws_qkv holds the prefill QKV rows, the pair of h, or (widths off 32) the gate and up halves side
-        // by side; ws_attn and ws_h belong to calls of one token per sequence
-        const size_t wide = std::max<size_t>(std::max<size_t>(s->qkv_rows, s->H % 32 ? 2 * (size_t)s->F : 0),
-                                             (size_t)pair_ld(s->F) / 2);
+        // ws_attn and ws_h belong to calls of one token per sequence
+        const size_t wide = wide_floats(s), pair = pair_elems(s);
         const size_t seqs = std::min<size_t>(rows, kMaxSeqs);
-        const size_t pair = (size_t)pair_ld(std::max<size_t>(std::max<size_t>(s->H, qd), s->F));
         if (hipMalloc(&s->ws_qkv, rows * wide * sizeof(float)) != hipSuccess ||
             hipMalloc(&s->ws_pair, rows * pair * sizeof(uint16_t)) != hipSuccess ||
             hipMalloc(&s->ws_q, rows * qd * sizeof(float)) != hipSuccess ||
@@ -555,6 +589,111 @@ int ensure_workspace(stage *s, size_t rows, size_t need_part) {
     return STAGE_OK;
 }
 
+// Whether the QKV product goes to memory, for what the rotation's kernels do not do themselves.
+bool plain_qkv(const stage *s) { return s->cfg.head_norm || s->cfg.max_adapters > 0; }
+bool has_ops(const stage *s) { return plain_qkv(s) || s->cfg.window > 0; }
+
+struct KvPool {   // the layer's cache as the operators take it
+    void *pool;
+    int kv_type;
+};
+KvPool kv_pool(const stage *s, int layer) {
+    return {static_cast<char *>(s->kv_pool) + (size_t)layer * s->kv_layer_stride, s->cfg.kv_fp32 ? STAGE_F32 : STAGE_BF16};
+}
+OpRows op_rows(const stage *s, int rows, int T, const RowMap &meta) {
+    OpRows r{};
+    r.table = s->d_table;
+    r.n_seqs = rows / T;
+    r.max_rows = T;
+    r.max_len = s->max_ctx;
+    r.max_blocks = s->max_blocks;
+    r.rows = rows;
+    r.n_blocks = s->n_blocks;
+    r.map = meta;
+    return r;
+}
+WindowArgs window_args(const stage *s, int layer, int rows, int T, const RowMap &meta) {
+    WindowArgs w{};
+    const KvPool kv = kv_pool(s, layer);
+    w.q = s->ws_q;
+    w.type = STAGE_F32;
+    w.q_ld = w.out_ld = (long)s->Hq * s->D;
+    w.pool = kv.pool;
+    w.kv_type = kv.kv_type;
+    w.n_q_heads = s->Hq;
+    w.n_kv_heads = s->Hkv;
+    w.head_dim = s->D;
+    w.window = s->cfg.window;
+    w.sinks = s->cfg.sinks;
+    w.scale = 1.f / std::sqrt((float)s->D);
+    w.rows = op_rows(s, rows, T, meta);
+    return w;
+}
+// Adapters of `target` over `rows` rows, their ids at the start of ws_ops.
+struct Projection { int in, out; };
+Projection projection(const stage *s, int target) {
+    const int qd = s->Hq * s->D;
+    return target == STAGE_ADAPT_QKV ? Projection{s->H, s->qkv_rows} : target == STAGE_ADAPT_O ? Projection{qd, s->H} : Projection{s->F, s->H};
+}
+AdapterArgs adapter_args(const stage *s, int target, int rows) {
+    const Projection p = projection(s, target);
+    AdapterArgs a{};
+    a.type = STAGE_F32;
+    a.rows = rows;
+    a.k = p.in;
+    a.n = p.out;
+    a.base_ld = a.out_ld = p.out;
+    a.n_adapters = s->cfg.max_adapters;
+    a.max_rank = s->cfg.adapter_rank;
+    return a;
+}
+// ws_ops of a call, in bytes: ids, then the states or sums of one launch at a time.
+size_t ops_sums(const stage *s, int rows) { return s->cfg.max_adapters ? align256((size_t)rows * sizeof(int)) : 0; }
+size_t ops_layout(const stage *s, int rows, int T, int longest) {
+    size_t most = 0;
+    if (s->cfg.window) {
+        WindowArgs w = window_args(s, 0, rows, T, RowMap{});
+        w.rows.max_len = longest;
+        most = window_workspace(w);
+    }
+    for (int t = 0; t < 3 && s->cfg.max_adapters; ++t) most = std::max(most, adapter_workspace(adapter_args(s, t, rows)));
+    return ops_sums(s, rows) + align256(most);
+}
+int ensure_ops(stage *s, int rows, int T) {
+    // (the longest context at once, so that it does not grow with every call of a sequence)
+    const size_t now = ops_layout(s, rows, T, s->max_ctx), need = std::max(now, ops_layout(s, rows, T, s->cfg.max_context));
+    if (now <= s->ops_bytes) return STAGE_OK;
+    int rc = sync_all(s);
+    if (rc) return rc;
+    if (s->ws_ops) (void)hipFree(s->ws_ops);
+    s->ws_ops = nullptr;
+    s->ops_bytes = 0;
+    if (hipMalloc(&s->ws_ops, need) != hipSuccess) {
+        (void)hipGetLastError();
+        return s->fail(STAGE_ENOMEM, "workspace for %d rows does not fit", rows);
+    }
+    s->ops_bytes = need;
+    return STAGE_OK;
+}
+
+// out += what the rows' adapters of a projection add (x: fp32 rows or the pair of a GEMM operand).
+int run_adapters(stage *s, int layer, int target, int rows, const void *x, long x_ld, bool x_pair, float *out) {
+    const Adapters &d = s->layers[layer].adapters[target];
+    if (d.n_set == 0) return STAGE_OK;
+    AdapterArgs a = adapter_args(s, target, rows);
+    a.x = x;
+    a.x_ld = x_ld;
+    a.x_pair = x_pair;
+    a.base = a.out = out;
+    a.a = d.a;
+    a.b = d.b;
+    a.ranks = d.ranks;
+    a.scales = d.scales;
+    a.ids = static_cast<const int *>(s->ws_ops);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(s->ws_ops) + ops_sums(s, rows));
+    HIP_TRY(launch_adapter_add(a, s->cs));
+    return STAGE_OK;
+}
 int ensure_dense(stage *s, size_t bytes) {
     if (bytes <= s->ws_dense_bytes) return STAGE_OK;
     int rc = sync_all(s);
@@ -804,9 +943,53 @@ RopeKvArgs rope_args(stage *s, int layer, int rows, const RowMap &meta) {
     return r;
 }
 
-// Prefill (T >= 2): projections on the matrix cores with bf16 hi/lo operand pairs.
+// The QKV product's n_part parts at `qkv`: norm of the heads, rotation, keys and values to the cache.
+int run_append(stage *s, int layer, const LayerWeights &w, int rows, int T, const RowMap &meta, float *qkv, int n_part) {
+    AppendArgs a{};
+    const KvPool kv = kv_pool(s, layer);
+    a.qkv = qkv;
+    a.qkv_type = STAGE_F32;
+    a.n_part = n_part;
+    a.part_stride = (size_t)rows * s->qkv_rows;
+    a.qkv_ld = s->qkv_rows;
+    a.q_out = s->ws_q;
+    a.q_type = STAGE_F32;
+    a.q_ld = (long)s->Hq * s->D;
+    if (s->cfg.head_norm) {
+        a.q_gain = w.mha + s->off_gq / 2;
+        a.k_gain = w.mha + s->off_gk / 2;
+    }
+    a.eps = s->cfg.rms_eps;
+    a.cos_t = s->d_cos;
+    a.sin_t = s->d_sin;
+    a.n_angles = s->cfg.max_context;
+    a.axis1 = a.axis2 = s->D / 2;
+    a.pool = kv.pool;
+    a.n_q_heads = s->Hq;
+    a.n_kv_heads = s->Hkv;
+    a.head_dim = s->D;
+    a.kv_type = kv.kv_type;
+    a.n_rows = rows;
+    a.rows = op_rows(s, rows, T, meta);
+    HIP_TRY(launch_norm_rope_append(a, s->cs));
+    return STAGE_OK;
+}
+// `pair`: the output as the O projection's operand pair, else fp32 rows.
+int run_window(stage *s, int layer, int rows, int T, const RowMap &meta, void *out, bool pair) {
+    WindowArgs w = window_args(s, layer, rows, T, meta);
+    w.out = out;
+    w.pair_rows = pair ? rows : 0;
+    w.part = reinterpret_cast<float *>(static_cast<char *>(s->ws_ops) + ops_sums(s, rows));
+    HIP_TRY(launch_window_attention(w, s->cs));
+    return STAGE_OK;
+}
+
+AttnArgs decode_attn_args(stage *s, int layer, int rows, const RowMap &meta, int grid_splits);
+
+// Prefill (T >= 2, and with the operators decode calls of many rows): projections on the matrix cores with bf16 hi/lo
+// operand pairs.
 int run_layer_prefill(stage *s, int layer, const LayerWeights &w, int rows, int T, const RowMap &meta,
-                      int key_ranges, const float *x_src, float *x_dst) {
+                      int key_ranges, const float *x_src, float *x_dst, const TimeRec &rec = {}) {
     const uint16_t *base = w.mha;
     const int H = s->H, F = s->F, qd = s->Hq * s->D;
     const float eps = s->cfg.rms_eps;
@@ -818,25 +1001,42 @@ int run_layer_prefill(stage *s, int layer, const LayerWeights &w, int rows, int 
     q.out = s->ws_qkv; q.ldo = s->qkv_rows;
     q.M = rows; q.N = s->qkv_rows; q.K = H;
     q.part = s->ws_split; q.part_cap64 = gemv_part_floats(s);
-    HIP_TRY(launch_qkv(q, rope_args(s, layer, rows, meta), s->cs));
+    int rc = STAGE_OK;
+    if (plain_qkv(s)) {
+        float *qkv = nullptr;
+        int n_part = 0;
+        HIP_TRY(launch_qkv_product(q, &qkv, &n_part, s->cs));
+        if ((rc = run_adapters(s, layer, STAGE_ADAPT_QKV, rows, s->ws_pair, pair_ld(H), true, qkv))) return rc;
+        if ((rc = run_append(s, layer, w, rows, T, meta, qkv, n_part))) return rc;
+    } else {
+        HIP_TRY(launch_qkv(q, rope_args(s, layer, rows, meta), s->cs));
+    }
 
-    AttnArgs at{};
-    at.q = s->ws_q;
-    at.kv = kv_view(s, layer);
-    at.n_q_heads = s->Hq;
-    at.kv_fp32 = s->cfg.kv_fp32;
-    at.rows = rows;
-    at.part_o = s->ws_part_o;
-    at.part_ml = s->ws_part_ml;
-    at.split_keys = 0;
-    at.max_splits = at.grid_splits = key_ranges;
-    at.n_seqs = rows / T;
-    at.rows_per_seq = T;
-    at.meta = meta;
-    at.out_pair = s->ws_pair;   // the O projection's operand pair
-    at.out_pair_ld = pair_ld(qd);
-    at.pair_rows = rows;
-    HIP_TRY(launch_attention(at, s->cs));
+    if (s->cfg.window) {
+        if ((rc = run_window(s, layer, rows, T, meta, s->ws_pair, true))) return rc;
+    } else {
+        AttnArgs at{};
+        if (T == 1) {
+            at = decode_attn_args(s, layer, rows, meta, key_ranges);
+        } else {
+            at.q = s->ws_q;
+            at.kv = kv_view(s, layer);
+            at.n_q_heads = s->Hq;
+            at.kv_fp32 = s->cfg.kv_fp32;
+            at.rows = rows;
+            at.part_o = s->ws_part_o;
+            at.part_ml = s->ws_part_ml;
+            at.split_keys = 0;
+            at.max_splits = at.grid_splits = key_ranges;
+            at.n_seqs = rows / T;
+            at.rows_per_seq = T;
+            at.meta = meta;
+        }
+        at.out_pair = s->ws_pair;   // the O projection's operand pair
+        at.out_pair_ld = pair_ld(qd);
+        at.pair_rows = rows;
+        HIP_TRY(launch_attention(at, s->cs));
+    }
 
     GemmArgs o{};
     o.a = s->ws_pair; o.lda = pair_ld(qd);
@@ -845,9 +1045,10 @@ int run_layer_prefill(stage *s, int layer, const LayerWeights &w, int rows, int 
     o.M = rows; o.N = H; o.K = qd;
     o.part = s->ws_split; o.part_cap64 = gemv_part_floats(s);
     HIP_TRY(launch_gemm(GEMM_RESIDUAL, o, 1, s->cs));
+    if ((rc = run_adapters(s, layer, STAGE_ADAPT_O, rows, s->ws_pair, pair_ld(qd), true, x_dst))) return rc;
 
     base = w.mlp;
-    int rc = mlp_boundary(s, layer, w);
+    rc = mlp_boundary(s, layer, w);
     if (rc) return rc;
     HIP_TRY(launch_rmsnorm_split(x_dst, base + s->off_g2 / 2, eps, rows, H, s->ws_pair, pair_ld(H), s->cs));
     GemmArgs gu{};
@@ -856,6 +1057,7 @@ int run_layer_prefill(stage *s, int layer, const LayerWeights &w, int rows, int 
     gu.w[1] = base + s->off_wu / 2;
     gu.M = rows; gu.N = F; gu.K = H;
     const uint16_t *h = s->ws_pair;   // h = silu(Wg y) * (Wu y) as a bf16 pair
+    if (rec.a) HIP_TRY(hipEventRecord(rec.a, s->cs));
     if (H % 32 == 0) {
         // SwiGLU and the hi/lo split in the GEMM's epilogue; the GEMM still reads the pair of y
         // from ws_pair, so h goes to the (fp32-sized) QKV workspace
@@ -869,6 +1071,7 @@ int run_layer_prefill(stage *s, int layer, const LayerWeights &w, int rows, int 
         HIP_TRY(launch_gemm(GEMM_STORE, gu, 2, s->cs));
         HIP_TRY(launch_swiglu_split(s->ws_qkv, F, rows, s->ws_pair, pair_ld(F), s->cs));
     }
+    if (rec.b) HIP_TRY(hipEventRecord(rec.b, s->cs));
 
     GemmArgs dn{};
     dn.a = h; dn.lda = pair_ld(F);
@@ -877,7 +1080,7 @@ int run_layer_prefill(stage *s, int layer, const LayerWeights &w, int rows, int 
     dn.M = rows; dn.N = H; dn.K = F;
     dn.part = s->ws_split; dn.part_cap64 = gemv_part_floats(s);
     HIP_TRY(launch_gemm(GEMM_RESIDUAL, dn, 1, s->cs));
-    return STAGE_OK;
+    return run_adapters(s, layer, STAGE_ADAPT_DOWN, rows, h, pair_ld(F), true, x_dst);
 }
 
 // The bf16 cache is read non-temporally by decode calls where all that the stage's sequences hold is more than
@@ -1075,19 +1278,39 @@ int run_layer_kernels(stage *s, int layer, const LayerWeights &w, int rows, int 
         rec.b = pooled_event(s);
         if (!rec.a || !rec.b) return s->fail(STAGE_EHIP, "hipEventCreate failed");
     }
-    if (decode_by_gemm(s, rows)) {
-        const int rc = run_layer_rows(s, layer, w, rows, meta, grid_splits, x_src, x_dst, rec);
+    if (has_ops(s) ? rows > kGemvRows : decode_by_gemm(s, rows)) {
+        const int rc = has_ops(s) ? run_layer_prefill(s, layer, w, rows, 1, meta, grid_splits, x_src, x_dst, rec)
+                                  : run_layer_rows(s, layer, w, rows, meta, grid_splits, x_src, x_dst, rec);
         if (rc == STAGE_OK && rec.a) s->recs.push_back(rec);
         return rc;
     }
-    const LayerGemvs g = layer_gemvs(s, layer, w, 0, rows, meta, x_src, x_dst);
-    HIP_TRY(launch_gemv(GEMV_NORM_ROPE_KV, g.q, s->cs));
-    HIP_TRY(launch_attention(decode_attn_args(s, layer, rows, meta, grid_splits), s->cs));
+    LayerGemvs g = layer_gemvs(s, layer, w, 0, rows, meta, x_src, x_dst);
+    int rc = STAGE_OK;
+    const int qd = s->Hq * s->D;
+    if (plain_qkv(s)) {
+        g.q.out = s->ws_qkv;
+        g.q.out_ld = s->qkv_rows;
+        HIP_TRY(launch_gemv(GEMV_NORM_STORE, g.q, s->cs));
+        if (s->layers[layer].adapters[STAGE_ADAPT_QKV].n_set) {   // (the GEMV keeps the normalised input to itself)
+            HIP_TRY(launch_rmsnorm_split(x_src, g.q.gain, s->cfg.rms_eps, rows, s->H, s->ws_pair, pair_ld(s->H), s->cs));
+            if ((rc = run_adapters(s, layer, STAGE_ADAPT_QKV, rows, s->ws_pair, pair_ld(s->H), true, s->ws_qkv))) return rc;
+        }
+        if ((rc = run_append(s, layer, w, rows, 1, meta, s->ws_qkv, 1))) return rc;
+    } else {
+        HIP_TRY(launch_gemv(GEMV_NORM_ROPE_KV, g.q, s->cs));
+    }
+    if (s->cfg.window) {
+        if ((rc = run_window(s, layer, rows, 1, meta, s->ws_attn, false))) return rc;
+    } else {
+        HIP_TRY(launch_attention(decode_attn_args(s, layer, rows, meta, grid_splits), s->cs));
+    }
     HIP_TRY(launch_gemv(GEMV_PLAIN_RESIDUAL, g.o, s->cs));
-    int rc = mlp_boundary(s, layer, w);
+    if ((rc = run_adapters(s, layer, STAGE_ADAPT_O, rows, s->ws_attn, qd, false, x_dst))) return rc;
+    rc = mlp_boundary(s, layer, w);
     if (rc) return rc;
     HIP_TRY(launch_gemv(GEMV_NORM_SWIGLU, g.gu, s->cs, rec.a, rec.b));
     HIP_TRY(launch_gemv(GEMV_PLAIN_RESIDUAL, g.dn, s->cs));
+    if ((rc = run_adapters(s, layer, STAGE_ADAPT_DOWN, rows, s->ws_h, s->F, false, x_dst))) return rc;
     if (rec.a) s->recs.push_back(rec);
     return STAGE_OK;
 }
@@ -1192,6 +1415,8 @@ int run_call_body(stage *s, int n_mb, const int32_t *mb_ids, int B, int T, const
     const size_t states = T == 1 ? s->max_splits : grid_splits > 1 ? prefill_key_ranges(1, 1, c.max_context, s->Hq, s->Hkv, true) : 0;
     int rc = ensure_workspace(s, rows, (rows * states + s->max_splits - 1) / s->max_splits);
     if (rc) return rc;
+    s->max_ctx = max_ctx;
+    if (has_ops(s) && (rc = ensure_ops(s, (int)rows, T))) return rc;
     // A zero-copy call with one token per sequence runs offloaded layers on their host blobs and
     // stages nothing; in zero-copy mode the slots are allocated by the first call that stages.
     const bool direct = c.zero_copy && T == 1;
@@ -1243,6 +1468,11 @@ int run_call_body(stage *s, int n_mb, const int32_t *mb_ids, int B, int T, const
     }
     const RowMap row_map{meta.n_seqs > 1 ? s->d_meta : nullptr, T, meta.seq_slot[0], meta.pos0[0]};
     if (row_map.seqs) HIP_TRY(launch_meta_write(meta, s->d_meta, s->cs));
+    if (c.max_adapters) {
+        SeqAdapters of{};
+        for (size_t i = 0; i < slots.size(); ++i) of.id[i] = s->adapter_of[slots[i]];
+        HIP_TRY(launch_adapter_rows(of, (int)rows, T, static_cast<int *>(s->ws_ops), s->cs));
+    }
     s->calls++;
     if (decode) s->tok_decode += (long long)rows; else s->tok_prefill += (long long)rows;
 
@@ -1326,10 +1556,11 @@ int run_call_body(stage *s, int n_mb, const int32_t *mb_ids, int B, int T, const
 // aligned; `split` and `split_ss` only for calls of 3 rows or more (the matrix-core projections).
 struct ScratchLayout {
     size_t meta = 0, q = 0, attn = 0, h = 0, part_o = 0, part_ml = 0, split = 0, split_ss = 0, total = 0;
+    size_t qkv = 0, pair = 0, ops = 0, ops_bytes = 0;   // with the operators only
     bool has_split = false;
 };
 
-ScratchLayout scratch_layout(const stage *s, size_t rows, int splits) {
+ScratchLayout scratch_layout(const stage *s, size_t rows, int splits, int longest) {
     ScratchLayout p;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -1348,6 +1579,12 @@ ScratchLayout scratch_layout(const stage *s, size_t rows, int splits) {
     if (p.has_split) {
         p.split = take(sizeof(float) * gemv_part_floats(s));
         p.split_ss = take(sizeof(float) * kGemvMaxSplits * 16);
+    }
+    if (has_ops(s)) {
+        p.ops_bytes = ops_layout(s, (int)rows, 1, longest);
+        p.qkv = take(rows * wide_floats(s) * sizeof(float));
+        p.pair = take(rows * pair_elems(s) * sizeof(uint16_t));
+        p.ops = take(p.ops_bytes);
     }
     p.total = off;
     return p;
@@ -1399,7 +1636,14 @@ int stage_init(const stage_config *cfg, stage **out) {
                         (c.timing & ~kTimeAll) == 0 && (c.zero_copy == 0 || c.zero_copy == 1) &&
                         c.kv_park_tokens >= 0 && c.kv_park_tokens <= c.max_context && c.n_lanes >= 0 &&
                         c.n_lanes <= STAGE_MAX_LANES && c.slot_check >= 0 && c.slot_check <= 2;
-    if (!shape_ok || !cap_ok) return STAGE_EINVAL;
+    const int group = shape_ok ? c.n_q_heads / c.n_kv_heads : 0;
+    const bool ops = c.head_norm || c.window || c.sinks || c.max_adapters || c.adapter_rank;
+    const bool ops_ok = !ops || ((c.head_norm == 0 || c.head_norm == 1) && c.window >= 0 && c.sinks >= 0 &&
+                                 (c.window > 0 || c.sinks == 0) && (c.max_adapters > 0) == (c.adapter_rank > 0) &&
+                                 c.max_adapters >= 0 && c.max_adapters <= kMaxAdapters &&
+                                 c.adapter_rank <= STAGE_OPS_MAX_RANK && c.adapter_rank % 4 == 0 &&
+                                 (c.head_dim == 64 || c.head_dim == 128) && group <= 8 && (group & (group - 1)) == 0);
+    if (!shape_ok || !cap_ok || !ops_ok) return STAGE_EINVAL;
     if (c.plan_mode != 0 && c.plan_mode != 1) return STAGE_EINVAL;
     for (int i = 0; i < c.n_thresholds; ++i) {
         if (c.thresholds[i] < (c.plan_mode ? 0 : 1) || (i > 0 && c.thresholds[i] < c.thresholds[i - 1]))
@@ -1423,6 +1667,10 @@ int stage_init(const stage_config *cfg, stage **out) {
     s->off_wqkv = off; off = align256(off + (size_t)s->qkv_rows * H * 2);
     s->off_wo = off;   off = align256(off + H * qd * 2);
     s->off_g1 = off;   off = align256(off + H * 2);
+    if (c.head_norm) {
+        s->off_gq = off;   off = align256(off + s->D * 2);
+        s->off_gk = off;   off = align256(off + s->D * 2);
+    }
     s->blk_bytes[kMha] = off;
     off = 0;         // MLP block
     s->off_wg = off;   off = align256(off + F * H * 2);
@@ -1443,6 +1691,7 @@ int stage_init(const stage_config *cfg, stage **out) {
     s->tables.assign(s->n_seq_slots, {});
     s->lengths.assign(s->n_seq_slots, 0);
     s->parked.assign(s->n_seq_slots, 0);
+    s->adapter_of.assign(s->n_seq_slots, -1);
     s->park_host.assign(s->n_seq_slots, nullptr);
     s->park_host_dev.assign(s->n_seq_slots, nullptr);
     s->ready_ev.assign(s->n_seq_slots, nullptr);
@@ -1521,8 +1770,10 @@ int stage_destroy(stage *s) {
     if (s->xs) (void)hipStreamSynchronize(s->xs);
     for (LaneState &ln : s->lanes)
         if (ln.cs) (void)hipStreamSynchronize(ln.cs);
-    for (Layer &l : s->layers)
+    for (Layer &l : s->layers) {
         for (Block &k : l.blk) free_block(k);
+        for (Adapters &d : l.adapters) free_adapters(d);
+    }
     for (void *p : s->slots) (void)hipFree(p);
     for (auto &v : s->slot_ready)
         for (hipEvent_t e : v) (void)hipEventDestroy(e);
@@ -1541,14 +1792,14 @@ int stage_destroy(stage *s) {
                     (void *)s->ws_qkv, (void *)s->ws_q, (void *)s->ws_attn, (void *)s->ws_h,
                     (void *)s->ws_pair,
                     (void *)s->ws_part_o, (void *)s->ws_part_ml, (void *)s->ws_split, (void *)s->ws_split_ss,
-                    s->ws_dense, (void *)s->d_slot_tags, (void *)s->d_slot_rec})
+                    s->ws_ops, s->ws_dense, (void *)s->d_slot_tags, (void *)s->d_slot_rec})
         if (p) (void)hipFree(p);
     if (s->own_cs && s->cs) (void)hipStreamDestroy(s->cs);
     if (s->own_xs && s->xs) (void)hipStreamDestroy(s->xs);
     for (LaneState &ln : s->lanes) {
         for (void *p : {(void *)ln.d_meta, (void *)ln.ws_qkv, (void *)ln.ws_q, (void *)ln.ws_attn, (void *)ln.ws_h,
                         (void *)ln.ws_pair, (void *)ln.ws_part_o, (void *)ln.ws_part_ml,
-                        (void *)ln.ws_split, (void *)ln.ws_split_ss})
+                        (void *)ln.ws_split, (void *)ln.ws_split_ss, ln.ws_ops})
             if (p) (void)hipFree(p);
         if (ln.own_cs && ln.cs) (void)hipStreamDestroy(ln.cs);
     }
@@ -1571,9 +1822,11 @@ int stage_load_layer(stage *s, int32_t layer, const stage_layer_weights *w, int3
         if (rc == STAGE_OK) s->base_code[layer] = resident;
         return rc;
     }
-    const void *src[9] = {w->wq, w->wk, w->wv, w->wo, w->wg, w->wu, w->wd, w->g1, w->g2};
-    for (const void *p : src)
-        if (!p) return s->fail(STAGE_EINVAL, "null weight pointer");
+    const int n = s->cfg.head_norm ? 11 : 9;   // (without it gq and gk are not read)
+    const void *src[11] = {w->wq, w->wk, w->wv, w->wo, w->wg, w->wu, w->wd, w->g1, w->g2,
+                           n > 9 ? w->gq : nullptr, n > 9 ? w->gk : nullptr};
+    for (int i = 0; i < n; ++i)
+        if (!src[i]) return s->fail(STAGE_EINVAL, "null weight pointer");
     int rc = check_residency(s, layer, resident);
     if (rc) return rc;
     Block fresh[2];
@@ -1590,16 +1843,16 @@ int stage_load_layer(stage *s, int32_t layer, const stage_layer_weights *w, int3
         return rc;
     }
     const size_t H = s->H, F = s->F, qd = (size_t)s->Hq * s->D, kvd = (size_t)s->Hkv * s->D;
-    const int blk_of[9] = {kMha, kMha, kMha, kMha, kMlp, kMlp, kMlp, kMha, kMlp};
-    const size_t offs[9] = {s->off_wqkv, s->off_wqkv + qd * H * 2, s->off_wqkv + (qd + kvd) * H * 2,
-                            s->off_wo, s->off_wg, s->off_wu, s->off_wd, s->off_g1, s->off_g2};
-    const size_t bytes[9] = {qd * H * 2, kvd * H * 2, kvd * H * 2, H * qd * 2, F * H * 2,
-                             F * H * 2, H * F * 2, H * 2, H * 2};
+    const int blk_of[11] = {kMha, kMha, kMha, kMha, kMlp, kMlp, kMlp, kMha, kMlp, kMha, kMha};
+    const size_t offs[11] = {s->off_wqkv, s->off_wqkv + qd * H * 2, s->off_wqkv + (qd + kvd) * H * 2,
+                            s->off_wo, s->off_wg, s->off_wu, s->off_wd, s->off_g1, s->off_g2, s->off_gq, s->off_gk};
+    const size_t bytes[11] = {qd * H * 2, kvd * H * 2, kvd * H * 2, H * qd * 2, F * H * 2,
+                             F * H * 2, H * F * 2, H * 2, H * 2, (size_t)s->D * 2, (size_t)s->D * 2};
     // Copies on the compute stream, then waited for: a device-to-device hipMemcpy on the null stream
     // returns before it completes, and kernels on a non-blocking compute stream would not wait for it
     // (they could read a half-copied layer).
     hipError_t e = hipSuccess;
-    for (int i = 0; i < 9 && e == hipSuccess; ++i) {
+    for (int i = 0; i < n && e == hipSuccess; ++i) {
         const Block &k = fresh[blk_of[i]];
         char *dst = static_cast<char *>(k.resident ? k.dev : k.host);
         e = hipMemcpyAsync(dst + offs[i], src[i], bytes[i], hipMemcpyDefault, s->cs);
@@ -1615,6 +1868,64 @@ int stage_load_layer(stage *s, int32_t layer, const stage_layer_weights *w, int3
     }
     ly.loaded = true;
     s->base_code[layer] = resident;
+    return STAGE_OK;
+}
+
+int stage_load_adapter(stage *s, int32_t layer, int32_t target, int32_t id, int32_t rank, float scale, const void *a,
+                       const void *b) {
+    if (!s) return STAGE_EINVAL;
+    s->err.clear();
+    const int most = s->cfg.max_adapters, R = s->cfg.adapter_rank;
+    if (layer < 0 || layer >= s->L || target < STAGE_ADAPT_QKV || target > STAGE_ADAPT_DOWN || id < 0 || id >= most ||
+        rank < 0 || rank > R || !std::isfinite(scale) || (rank > 0 && (!a || !b)))
+        return s->fail(STAGE_EINVAL, "bad adapter (layer %d, target %d, id %d of %d, rank %d of %d)", layer, target, id, most,
+                       rank, R);
+    DeviceGuard dg(s->cfg.device);
+    int rc = sync_all(s);
+    if (rc) return rc;
+    Adapters &d = s->layers[layer].adapters[target];
+    const Projection p = projection(s, target);
+    const size_t a_elems = (size_t)R * p.in, b_elems = (size_t)p.out * R;
+    if (!d.a) {
+        Adapters fresh;
+        if (hipMalloc(&fresh.a, most * a_elems * 2) != hipSuccess || hipMalloc(&fresh.b, most * b_elems * 2) != hipSuccess ||
+            hipMalloc(&fresh.ranks, most * sizeof(int)) != hipSuccess || hipMalloc(&fresh.scales, most * sizeof(float)) != hipSuccess) {
+            (void)hipGetLastError();
+            free_adapters(fresh);
+            return s->fail(STAGE_ENOMEM, "the adapters of a projection do not fit");
+        }
+        fresh.set.assign(most, 0);
+        hipError_t e = hipMemsetAsync(fresh.ranks, 0, most * sizeof(int), s->cs);
+        if (e == hipSuccess) e = hipMemsetAsync(fresh.a, 0, most * a_elems * 2, s->cs);   // (what no adapter fills is read, too)
+        if (e == hipSuccess) e = hipMemsetAsync(fresh.b, 0, most * b_elems * 2, s->cs);
+        if (e == hipSuccess) e = hipStreamSynchronize(s->cs);
+        if (e != hipSuccess) {
+            free_adapters(fresh);
+            return s->fail_hip(e, "clearing adapters");
+        }
+        d = fresh;
+    }
+    hipError_t e = hipSuccess;
+    if (rank > 0) {
+        e = hipMemcpyAsync(d.a + id * a_elems, a, (size_t)rank * p.in * 2, hipMemcpyDefault, s->cs);
+        if (e == hipSuccess)
+            e = hipMemcpy2DAsync(d.b + id * b_elems, (size_t)R * 2, b, (size_t)rank * 2, (size_t)rank * 2, p.out, hipMemcpyDefault, s->cs);
+    }
+    if (e == hipSuccess) e = hipMemcpyAsync(d.scales + id, &scale, sizeof scale, hipMemcpyHostToDevice, s->cs);
+    if (e == hipSuccess) e = hipMemcpyAsync(d.ranks + id, &rank, sizeof rank, hipMemcpyHostToDevice, s->cs);
+    if (e == hipSuccess) e = hipStreamSynchronize(s->cs);
+    if (e != hipSuccess) return s->fail_hip(e, "copying an adapter");
+    d.n_set += (rank > 0) - (d.set[id] > 0);
+    d.set[id] = rank;
+    return STAGE_OK;
+}
+
+int stage_set_adapter(stage *s, int32_t mb, int32_t b, int32_t id) {
+    if (!s) return STAGE_EINVAL;
+    s->err.clear();
+    if (mb < 0 || mb >= s->cfg.max_microbatches || b < 0 || b >= s->cfg.max_batch || id < -1 || id >= s->cfg.max_adapters)
+        return s->fail(STAGE_EINVAL, "bad sequence (%d, %d) or adapter %d", mb, b, id);
+    s->adapter_of[seq_slot(s, mb, b)] = id;
     return STAGE_OK;
 }
 
@@ -1705,7 +2016,8 @@ int stage_decode_noalloc(stage *s, int32_t n_mb, const int32_t *mb_ids, int32_t 
         max_after = std::max(max_after, s->lengths[sl] + 1);
     }
     const int splits = std::min(s->max_splits, (max_after + kDecodeSplitKeys - 1) / kDecodeSplitKeys);
-    const ScratchLayout lay = scratch_layout(s, slots.size(), splits);
+    DeviceGuard dg(c.device);
+    const ScratchLayout lay = scratch_layout(s, slots.size(), splits, max_after);
     if (lay.total > kScratchBytes)
         return s->fail(STAGE_ENOMEM, "the call needs %zu bytes of scratch; the limit is %zu (STAGE_NOALLOC_SCRATCH_BYTES)",
                        lay.total, kScratchBytes);
@@ -1736,7 +2048,12 @@ int stage_decode_noalloc(stage *s, int32_t n_mb, const int32_t *mb_ids, int32_t 
     ws.ws_part_ml = reinterpret_cast<float *>(base + lay.part_ml);
     ws.ws_split = lay.has_split ? reinterpret_cast<float *>(base + lay.split) : nullptr;
     ws.ws_split_ss = lay.has_split ? reinterpret_cast<float *>(base + lay.split_ss) : nullptr;
-    DeviceGuard dg(c.device);
+    if (has_ops(s)) {
+        ws.ws_qkv = reinterpret_cast<float *>(base + lay.qkv);
+        ws.ws_pair = reinterpret_cast<uint16_t *>(base + lay.pair);
+        ws.ws_ops = base + lay.ops;
+        ws.ops_bytes = lay.ops_bytes;
+    }
     swap_workspaces(s, ws);
     const int saved_splits = s->max_splits;
     const int32_t timing = s->cfg.timing;
@@ -1837,6 +2154,7 @@ int stage_reset_sequence(stage *s, int32_t mb, int32_t b) {
     s->lengths[slot] = 0;
     s->parked[slot] = 0;
     s->ready_pending[slot] = 0;
+    s->adapter_of[slot] = -1;
     release_tail_blocks(s, slot);
     return STAGE_OK;
 }

@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256) void window_split(WindowArgs a, SplitPlan pl) 
         const size_t r = seq.first + t0 + ct;
         const int hc = (g << pl.log_g) + (col & ((1 << pl.log_g) - 1));
         if (pl.splits == 1) {
-            store4(a.out, r * a.out_ld + (size_t)hc * D + d, a.type, quotient(o, sum));
+            store4(a.out, r * a.out_ld + (size_t)hc * D + d, (long)r < a.pair_rows ? kPair : a.type, quotient(o, sum));
         } else {
             const size_t st = (r * a.n_q_heads + hc) * pl.splits + split;
             float *const ml = a.part + (size_t)a.rows.rows * a.n_q_heads * pl.splits * D;
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(256) void window_merge(WindowArgs a, SplitPlan pl) 
         const float4 o1 = make_float4(lane_xor(o.x, x), lane_xor(o.y, x), lane_xor(o.z, x), lane_xor(o.w, x));
         join(m1, l1, o1);
     }
-    if (sl == 0) store4(a.out, row * a.out_ld + (size_t)h * D + 4 * cg, a.type, quotient(o, l));
+    if (sl == 0) store4(a.out, row * a.out_ld + (size_t)h * D + 4 * cg, (long)row < a.pair_rows ? kPair : a.type, quotient(o, l));
 }
 
 SplitPlan split_plan(const WindowArgs &a) {
@@ -799,12 +799,13 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
     constexpr int E = TYPE == STAGE_F32 ? 4 : 2, OROW = D * E + 16, OCH = D * E / 16;
     static_assert(64 + 4 * 32 * OROW <= S * L::BYTES, "the ring holds the output rows");
     char *const out_lds = lds + 64 + wave * 32 * OROW;   // (behind the flags)
+    const int out_type = TYPE == STAGE_F32 && seq.first + t0 + t < a.pair_rows ? kPair : TYPE;
     const float sum = l + lane_xor(l, 32);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, TYPE,
+            store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, out_type,
                    quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
 #pragma unroll
     for (int i = 0; i < 32 * OCH / 64; ++i) {

@@ -222,13 +222,14 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
     }
     auto store = [&] {
         const float sum = l + lane_xor(l, 32);
+        const int out_type = TYPE == STAGE_F32 && seq.first + t0 + row < a.pair_rows ? kPair : TYPE;
         if (row < rows) {
             const size_t to = (size_t)(seq.first + t0 + row) * a.out_ld + at - 8 * half;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    store4(a.out, to + 32 * b + 8 * j + 4 * half, TYPE,
+                    store4(a.out, to + 32 * b + 8 * j + 4 * half, out_type,
                            quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
         }
     };

@@ -6,6 +6,7 @@
 
 #include "lanes.h"
 #include "ops_kernels.h"
+#include "pair.h"
 #include "stage_ops.h"
 
 namespace stg {
@@ -68,8 +69,12 @@ __device__ __forceinline__ void load4(const void *p, size_t e, int type, float v
         v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xFFFF0000u);
     }
 }
+// (kPair: rows of a multiple of 32 elements, so the pair of element e of many rows is at pair_at(e))
+constexpr int kPair = -1;
 __device__ __forceinline__ void store4(void *p, size_t e, int type, float4 v) {
-    if (type == STAGE_F32) {
+    if (type == kPair) {
+        store_pair4(static_cast<uint16_t *>(p) + pair_at((long)e), v);
+    } else if (type == STAGE_F32) {
         *reinterpret_cast<float4 *>(static_cast<float *>(p) + e) = v;
     } else {
         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));

@@ -37,11 +37,12 @@ EXPORTED = (
     "stage_get_block_table", "stage_get_length", "stage_get_residency", "stage_get_slot_log",
     "stage_get_demotion_log", "stage_get_residency_log", "stage_get_timeline", "stage_set_timing", "stage_get_stats",
     "stage_last_error", "stage_strerror", "stage_plan_offload", "stage_allocate", "stage_kv_park", "stage_kv_unpark",
-    "stage_decode_noalloc",
+    "stage_decode_noalloc", "stage_load_adapter", "stage_set_adapter",
     "stage_norm_rope_append", "stage_window_workspace", "stage_window_attention", "stage_adapter_workspace",
     "stage_adapter_add",
 )
 STAGE_F32, STAGE_BF16 = 0, 1
+STAGE_ADAPT_QKV, STAGE_ADAPT_O, STAGE_ADAPT_DOWN = 0, 1, 2
 STAGE_OPS_MAX_ROWS, STAGE_OPS_MAX_BLOCKS = 1048560, 1048576
 STAGE_OPS_MAX_SEQS = 65536
 STAGE_OPS_MAX_RANK = 256
@@ -65,6 +66,8 @@ class StageConfig(ctypes.Structure):
         ("plan_beta", c_int32 * STAGE_MAX_THRESHOLDS), ("kv_park_tokens", c_int32),
         ("n_lanes", c_int32), ("lane_streams", c_void_p * STAGE_MAX_LANES),
         ("slot_check", c_int32),
+        ("head_norm", c_int32), ("window", c_int32), ("sinks", c_int32),
+        ("max_adapters", c_int32), ("adapter_rank", c_int32),
     ]
 
 
@@ -97,7 +100,7 @@ class StageAllocPlan(ctypes.Structure):
 
 
 class StageLayerWeights(ctypes.Structure):
-    _fields_ = [(n, c_void_p) for n in ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2")]
+    _fields_ = [(n, c_void_p) for n in ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2", "gq", "gk")]
 
 
 class StageError(RuntimeError):
@@ -124,6 +127,8 @@ def lib():
         "stage_init": (c_int32, [POINTER(StageConfig), POINTER(c_void_p)]),
         "stage_destroy": (c_int32, [c_void_p]),
         "stage_load_layer": (c_int32, [c_void_p, c_int32, POINTER(StageLayerWeights), c_int32]),
+        "stage_load_adapter": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p]),
+        "stage_set_adapter": (c_int32, [c_void_p, c_int32, c_int32, c_int32]),
         "stage_prefill": (c_int32, [c_void_p, c_int32, ip, c_int32, c_int32, c_void_p, c_void_p]),
         "stage_decode": (c_int32, [c_void_p, c_int32, ip, c_int32, c_void_p, c_void_p]),
         "stage_decode_lane": (c_int32, [c_void_p, c_int32, c_int32, ip, c_int32, c_void_p, c_void_p]),
@@ -209,12 +214,30 @@ def stage_destroy(h) -> None:
 
 
 def stage_load_layer(h, layer: int, weights: Optional[Dict[str, object]], resident: int) -> None:
-    """weights: name -> bf16 bits (numpy uint16 or torch int16/bfloat16, host or device), or None."""
+    """weights: name -> bf16 bits (numpy uint16 or torch int16/bfloat16, host or device), or None; gq and gk with
+    head_norm."""
     if weights is None:
         _check(lib().stage_load_layer(h, layer, None, int(resident)), h)
         return
-    w = StageLayerWeights(*[_ptr(weights[n]) for n in ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2")])
+    w = StageLayerWeights(*[_ptr(weights[n]) for n in ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2")],
+                          *[_ptr(weights[n]) for n in ("gq", "gk") if n in weights])
     _check(lib().stage_load_layer(h, layer, ctypes.byref(w), int(resident)), h)
+
+
+def stage_load_adapter(h, layer: int, target: int, id: int, a, b, scale: float = 1.0) -> None:
+    """Adapter ``id`` of a layer's projection (STAGE_ADAPT_*): a [rank, in], b [out, rank], bf16 bits as for
+    stage_load_layer; None for both takes it out."""
+    if a is None and b is None:
+        _check(lib().stage_load_adapter(h, layer, target, id, 0, 0.0, None, None), h)
+        return
+    if a.ndim != 2 or b.ndim != 2 or b.shape[1] != a.shape[0] or a.shape[0] < 1:
+        raise ValueError("a is [rank, in], b [out, rank]")
+    _check(lib().stage_load_adapter(h, layer, target, id, a.shape[0], scale, _ptr(a), _ptr(b)), h)
+
+
+def stage_set_adapter(h, mb: int, b: int, id: int) -> None:
+    """The adapter of sequence (mb, b) in later calls; -1: none."""
+    _check(lib().stage_set_adapter(h, mb, b, id), h)
 
 
 def stage_prefill(h, mb_ids: Sequence[int], B: int, T: int, x_in: torch.Tensor, x_out: torch.Tensor) -> None:
@@ -355,11 +378,13 @@ def config_for(shape, *, max_microbatches: int, max_batch: int, max_context: int
                kv_pool_blocks: int = 0, device: int = 0, compute_stream=None, copy_stream=None,
                timing: int = 0, zero_copy: bool = False,
                plan: Optional[Sequence[Tuple[int, int, int]]] = None, kv_park_tokens: int = 0,
-               n_lanes: int = 1, lane_streams: Optional[Sequence] = None, slot_check: int = 0) -> StageConfig:
+               n_lanes: int = 1, lane_streams: Optional[Sequence] = None, slot_check: int = 0, head_norm: bool = False,
+               window: int = 0, sinks: int = 0, max_adapters: int = 0, adapter_rank: int = 0) -> StageConfig:
     """A StageConfig for a stage shape (any object with the StageShape fields).  ``plan``:
     planner steps [(tokens, alpha, beta)] (plan_mode 1), instead of ``thresholds``.
     ``n_lanes`` decode lanes; ``lane_streams[l]``: lane l's stream handle (None: the library's).
-    ``slot_check``: the slot tag check mode (0 off, 1 on, 2 self-test)."""
+    ``slot_check``: the slot tag check mode (0 off, 1 on, 2 self-test).  ``head_norm``, ``window``, ``sinks``,
+    ``max_adapters`` and ``adapter_rank``: what the attention block has beyond the plain one."""
     cfg = stage_config_default()
     cfg.n_layers, cfg.hidden = shape.n_layers, shape.hidden
     cfg.n_q_heads, cfg.n_kv_heads = shape.n_q_heads, shape.n_kv_heads
@@ -391,4 +416,7 @@ def config_for(shape, *, max_microbatches: int, max_batch: int, max_context: int
     for l, st in enumerate(lane_streams or ()):
         cfg.lane_streams[l] = st
     cfg.slot_check = slot_check
+    cfg.head_norm = int(bool(head_norm))
+    cfg.window, cfg.sinks = window, sinks
+    cfg.max_adapters, cfg.adapter_rank = max_adapters, adapter_rank
     return cfg
