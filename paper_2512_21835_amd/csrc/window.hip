@@ -45,7 +45,9 @@ struct PageLds {
     }
 };
 
-// One wavefront's attention of 16 columns over its pages.  Everything of it is the wavefront's own: no barrier.
+// One wavefront's attention of 16 columns over its pages.  Everything of it is the wavefront's own: no barrier.  All
+// fragments of a page's K, and later of its V, are read before the first of their MFMAs (read one by one between them, a
+// wavefront alone on its SIMD waits for each: 3 us instead of 1 for a page of 128 fp32).
 //
 // S^T = K Q^T: lane l holds keys 4 (l / 16) + i of the page for column l % 16, which is the layout of the operand P^T of
 // O^T += V^T P^T, so probabilities stay in registers; o[b][i]: d 16 b + 4 (l / 16) + i of column l % 16.  bf16 cache:
@@ -105,25 +107,29 @@ struct Columns {
         f32x4_t sc = {0.f, 0.f, 0.f, 0.f}, s1 = sc;
         const uint32_t kr = lds + l16 * L::ROW;
         if constexpr (F32) {
+            f32x4_t k[D / 16];
 #pragma unroll
-            for (int v = 0; v < D / 16; ++v) {
-                const f32x4_t k = __builtin_bit_cast(f32x4_t, *(lds16)(kr + 16 * ((4 * v + lq) ^ L::kx(l16))));
+            for (int v = 0; v < D / 16; ++v) k[v] = __builtin_bit_cast(f32x4_t, *(lds16)(kr + 16 * ((4 * v + lq) ^ L::kx(l16))));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int v = 0; v < D / 16; ++v)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    if (c & 1) s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c], qf[4 * v + c], s1, 0, 0, 0);
-                    else sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c], qf[4 * v + c], sc, 0, 0, 0);
+                    if (c & 1) s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[v][c], qf[4 * v + c], s1, 0, 0, 0);
+                    else sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[v][c], qf[4 * v + c], sc, 0, 0, 0);
                 }
-            }
         } else {
+            bf16x8_t k[D / 32];
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
-                const bf16x8_t k = __builtin_bit_cast(bf16x8_t, *(lds16)(kr + 16 * ((4 * s + lq) ^ L::kx(l16))));
+            for (int s = 0; s < D / 32; ++s) k[s] = __builtin_bit_cast(bf16x8_t, *(lds16)(kr + 16 * ((4 * s + lq) ^ L::kx(l16))));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s)
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) {
-                    if (t & 1) s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][s], s1, 0, 0, 0);
-                    else sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][s], sc, 0, 0, 0);
+                    if (t & 1) s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[s], q[t][s], s1, 0, 0, 0);
+                    else sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[s], q[t][s], sc, 0, 0, 0);
                 }
-            }
         }
         const float scale = a.scale * kLog2e;   // scores in base 2
         float p[4], top = -INFINITY;
@@ -153,16 +159,19 @@ struct Columns {
         const uint32_t vr = lds + L::HALF;
         if (masked) hide(a, vr, k0, first, rows, p);
         if constexpr (F32) {
+            float v[4][D / 16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = 4 * lq + i;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int b = 0; b < D / 16; ++b) {
-                    const int c = 4 * b + l16 / 4;
-                    const float v = *(lds4)(vr + key * L::ROW + 16 * (c ^ L::vx(key)) + 4 * (l16 & 3));
-                    o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[i], o[b], 0, 0, 0);
+                    const int key = 4 * lq + i, c = 4 * b + l16 / 4;
+                    v[i][b] = *(lds4)(vr + key * L::ROW + 16 * (c ^ L::vx(key)) + 4 * (l16 & 3));
                 }
-            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int b = 0; b < D / 16; ++b) o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][b], p[i], o[b], 0, 0, 0);
         } else {
             s16x4_t pt[TERMS];
 #pragma unroll
@@ -176,12 +185,15 @@ struct Columns {
             // + 3) column-wise: lane i all keys of d i
             const int key = 4 * lq + l16 / 4;
             const uint32_t at = vr + key * L::ROW + 8 * (l16 & 1);
+            s16x4_t v[D / 16];
 #pragma unroll
-            for (int b = 0; b < D / 16; ++b) {
-                const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)(at + 16 * ((2 * b + (l16 >> 1 & 1)) ^ L::vx(key))));
+            for (int b = 0; b < D / 16; ++b)
+                v[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)(at + 16 * ((2 * b + (l16 >> 1 & 1)) ^ L::vx(key))));
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < TERMS; ++j) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pt[j], o[b], 0, 0, 0);
-            }
+            for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[b], pt[j], o[b], 0, 0, 0);
         }
     }
 

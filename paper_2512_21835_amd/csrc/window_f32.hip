@@ -161,17 +161,26 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
         // (behind the last tile: what the registers hold goes to a stage that nobody reads)
-        constexpr int N = PL * KK;
+        // Fragments are read AHEAD groups of MFMAs before theirs (a wavefront alone on its SIMD waits for what it reads).
+        constexpr int N = PL * KK, AHEAD = 3;
+        bf16x8_t k[AHEAD];
+        auto key_frag = [&](int c) {   // plane PL - 1 - c % PL: small terms first
+            return __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + now + (PL - 1 - c % PL) * L::PLANE) ^ (32 * (c / PL))));
+        };
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c) k[c] = key_frag(c);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            const int kk = c / PL, p = PL - 1 - c % PL;   // (small terms first)
-            const bf16x8_t k = __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + now + p * L::PLANE) ^ (32 * kk)));
+            const int kk = c / PL, p = PL - 1 - c % PL;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = TERMS - 1; i >= 0; --i)
-                if (i + p < PL) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][kk], s, 0, 0, 0);
+                if (i + p < PL) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[c % AHEAD], q[i][kk], s, 0, 0, 0);
+            if (c + AHEAD < N) k[c % AHEAD] = key_frag(c + AHEAD);
 #pragma unroll
             for (int e = 0; e < PIECES; ++e)
                 if (e * N / PIECES == c) convert(next, e);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (t + 2 < n_tiles) fetch(t + 2);
         if (!clear.has(t) | strange) {
@@ -195,8 +204,12 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
         }
+        constexpr int M = 2 * PL * NB;
+        auto value_of = [&](int c) { return value_frag(v_at + now + (PL - 1 - c / NB % PL) * L::PLANE, c / NB / PL, c % NB); };
         const float ref = m == -INFINITY ? 0.f : m;
-        bf16x8_t p[TERMS][2];
+        bf16x8_t p[TERMS][2], v[AHEAD];
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c) v[c] = value_of(c);
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -209,16 +222,15 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         }
         l += sum;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int c = 0; c < M; ++c) {
+            const int pl = PL - 1 - c / NB % PL, h = c / NB / PL, b = c % NB;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int pl = PL - 1; pl >= 0; --pl)
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const bf16x8_t v = value_frag(v_at + now + pl * L::PLANE, h, b);
-#pragma unroll
-                    for (int i = TERMS - 1; i >= 0; --i)
-                        if (i + pl < PL) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i][h], o[b], 0, 0, 0);
-                }
+            for (int i = TERMS - 1; i >= 0; --i)
+                if (i + pl < PL) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c % AHEAD], p[i][h], o[b], 0, 0, 0);
+            if (c + AHEAD < M) v[c % AHEAD] = value_of(c + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     auto store = [&] {
         const float sum = l + lane_xor(l, 32);
