@@ -693,21 +693,20 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
             continue;
         }
         f32x16_t n;
-        bf16x8_t pn[TERMS][2], vf[2 * NB];
+        u32x4 pn[TERMS][2];
+        bf16x8_t vf[2 * NB];
         const float ref = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) n[i] = 0.f;
         auto softmax_piece = [&](int e) {   // scores 2 e and the one behind it
+            const float w0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale, -ref)), w1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale, -ref));
+            sum += w0;
+            sum += w1;
+            uint32_t w[TERMS];
+            cut_terms2<TERMS>(w0, w1, w);
 #pragma unroll
-            for (int i = 2 * e; i < 2 * e + 2; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
-                sum += w;
-                __bf16 b[TERMS];
-                split_terms<TERMS>(w, b);
-#pragma unroll
-                for (int j = 0; j < TERMS; ++j) pn[j][i / 8][i % 8] = b[j];
-            }
+            for (int j = 0; j < TERMS; ++j) pn[j][e / 4][e % 4] = w[j];
             asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)
         };
         __builtin_amdgcn_sched_barrier(0);
@@ -761,7 +760,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
 #pragma unroll
         for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) p[i][h] = pn[i][h];
+            for (int h = 0; h < 2; ++h) p[i][h] = __builtin_bit_cast(bf16x8_t, pn[i][h]);
         raise(top, p);
     }
     // whether any wavefront cleared a V

@@ -13,8 +13,8 @@ namespace {
 // O^T += V^T P^T with 32x32x16 MFMAs, lane l holding keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for column l % 32, the
 // k order of the operand P^T.
 //
-// fp32 rows: three terms of q and p against three planes hold all 24 bits of each; of the nine products the six whose terms are
-// 2^-16 of the largest or more are taken, which leaves 2^-24 each.  bf16 rows: q is its one term, p one rounding to bf16
+// fp32 rows: three terms of q and p against three planes hold all 24 bits of each; of the nine products the six largest are
+// taken; the others are at most 2^-23 of the whole.  bf16 rows: q is its one term, p one rounding to bf16
 // (2^-9 of a probability, as everywhere with bf16 rows) and two planes, 2^-17, are well below that.
 template <int D, int PL>
 struct PlaneLds {
@@ -23,9 +23,6 @@ struct PlaneLds {
     __device__ static int kx(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
     __device__ static int vx(int key) { return D == 128 ? (key & 3) << 2 : (key & 2) << 1; }
 };
-
-// Beyond this a number is no sum of finite bf16 terms.
-constexpr float kLargest = 0x1.FEp127f;
 
 template <int D, int TERMS, int PL>
 __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log_g) {
@@ -54,47 +51,50 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
     bool strange = __builtin_amdgcn_ballot_w64(!known(ids)) != 0;   // some page so far is not of the pool
 
     // The thread's part of a tile: key 8 wave + lane / 8, chunks lane % 8 + 8 i of K and of V.
-    f32x4_t raw[2][L::CHUNKS][2];
-    auto fetch = [&](int t) {   // (t ascending, each once)
+    f32x4_t raw_k[L::CHUNKS][2], raw_v[L::CHUNKS][2];
+    int block_k[2] = {0, 0};   // of the last two tiles whose K was fetched: V's turn comes two tiles later
+    auto fetch = [&](f32x4_t(&raw)[L::CHUNKS][2], int b, size_t of) {
+        const float *from = pool + (size_t)(known(b) ? b : 0) * block_elems + of + ((wave & 1) * 8 + lane / 8) * D + lane % 8 * 8;
+#pragma unroll
+        for (int i = 0; i < L::CHUNKS; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) raw[i][h] = *reinterpret_cast<const f32x4_t *>(from + 64 * i + 4 * h);
+    };
+    auto fetch_k = [&](int t) {   // (t ascending, each once)
+        block_k[0] = block_k[1];
+        if (t >= n_tiles) return;
         if (t > 0 && t % 32 == 0) {
             ids = more_ids;
             strange |= __builtin_amdgcn_ballot_w64(!known(ids)) != 0;
             more_ids = ids_from(t + 32);
         }
-        const int b = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
-        const float *from = pool + (size_t)(known(b) ? b : 0) * block_elems + ((wave & 1) * 8 + lane / 8) * D + lane % 8 * 8;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-            for (int i = 0; i < L::CHUNKS; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    raw[kv][i][h] = *reinterpret_cast<const f32x4_t *>(from + kv * hkv * head + 64 * i + 4 * h);
+        block_k[1] = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
+        fetch(raw_k, block_k[1], 0);
     };
-    // A K or V that is not finite, or too large for terms, becomes 0: the columns that see it are taken again at the end.
+    // A K or V that is not finite becomes 0: the columns that see it are taken again at the end.
     bool odd = false;
     const int my_key = 8 * wave + lane / 8;
     const uint32_t k_to = base + my_key * L::ROW + 16 * (lane % 8 ^ L::kx(my_key));
     const uint32_t v_to = base + L::HALF + my_key * L::ROW + 16 * (lane % 8 ^ L::vx(my_key));
-    bf16x8_t planes[PL];
-    constexpr int PIECES = 2 * L::CHUNKS * 4;   // two elements each
-    auto convert = [&](uint32_t stage, int piece) {
-        const int kv = piece / (4 * L::CHUNKS), i = piece / 4 % L::CHUNKS, e0 = piece % 4 * 2;
+    u32x4 planes[PL];
+    constexpr int PIECES = 4 * L::CHUNKS;   // two elements each
+    auto convert = [&](const f32x4_t(&raw)[L::CHUNKS][2], uint32_t to, int piece) {
+        const int i = piece / 4, e0 = piece % 4 * 2;
+        float x[2];
 #pragma unroll
-        for (int e = e0; e < e0 + 2; ++e) {
-            float x = raw[kv][i][e / 4][e % 4];
-            const bool bad = !(fabsf(x) <= kLargest);
+        for (int e = 0; e < 2; ++e) {
+            x[e] = raw[i][e0 / 4][e0 % 4 + e];
+            const bool bad = !(fabsf(x[e]) < INFINITY);
             odd |= bad;
-            x = bad ? 0.f : x;
-            __bf16 terms[PL];
-            split_terms<PL>(x, terms);
-#pragma unroll
-            for (int p = 0; p < PL; ++p) planes[p][e] = terms[p];
+            x[e] = bad ? 0.f : x[e];
         }
+        uint32_t w[PL];
+        cut_terms2<PL>(x[0], x[1], w);
+#pragma unroll
+        for (int p = 0; p < PL; ++p) planes[p][e0 / 2] = w[p];
         if (e0 == 6) {
 #pragma unroll
-            for (int p = 0; p < PL; ++p)
-                *(lds16)(((kv ? v_to : k_to) ^ (128 * i)) + stage + p * L::PLANE) = __builtin_bit_cast(u32x4, planes[p]);
+            for (int p = 0; p < PL; ++p) *(lds16)((to ^ (128 * i)) + p * L::PLANE) = planes[p];
         }
     };
 
@@ -104,7 +104,8 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
     const int r = c0 + col, row = r & (bq - 1), pos = row < rows ? first + row : -1;
     const size_t at = (size_t)((g << log_g) + (r >> log_bq)) * D + 8 * half;
     const size_t q_at = (size_t)(seq.first + t0 + min(row, rows - 1)) * a.q_ld + at;
-    if (n_tiles > 0) fetch(0);
+    fetch_k(0);
+    if (n_tiles > 0) fetch(raw_v, block_k[1], hkv * head);
     bf16x8_t q[TERMS][KK];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
@@ -136,101 +137,156 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     const Turns clear = rb.whole(a, w_first, max(w_first, w_last));
-    Turns mine = rb.touched(a, w_first, max(w_first, w_last));
+    Turns mine = widened(rb.touched(a, w_first, max(w_first, w_last)));   // what the wavefront takes part in
     if (w_rows <= 0) mine = Turns{0, 0, 0};
+    auto hide = [&](f32x16_t &x, int t) {
+        uint32_t pages = t < n_tiles ? ~0u : 0u;
+        if (strange && t < n_tiles)
+            pages = (known(seq.table[rb.page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[rb.page_at(t, 1)]) ? 0xFFFF0000u : 0u);
+        hide_scores(x, pages >> (4 * half) & seen_bits(a, pos, rb.tile_at(t) * kTileKeys + 4 * half));
+    };
+    bf16x8_t p[TERMS][2];   // probabilities of tile t - 1
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) p[i][h] = bf16x8_t{};
+    // The maximum: a whole number that stays until a score is 2^kSlack beyond it, so that rescaling is exact, and rare.
+    auto raise = [&](float top) {
+        const float best = fmaxf(top, lane_xor(top, 32)) * scale;
+        if (__builtin_amdgcn_ballot_w64(best > m + kSlack) == 0) return;
+        const float to = best > m + kSlack ? ceilf(best) : m;
+        const float alpha = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
+        m = to;
+        l *= alpha;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[i][h][j] = (__bf16)((float)p[i][h][j] * alpha);
+    };
+    // Groups of MFMAs of one fragment (small terms first), the fragments read AHEAD groups before theirs.
+    constexpr int N = PL * KK, M = 2 * PL * NB, AHEAD = PL;
+    auto key_frag = [&](uint32_t stage, int c) {
+        return __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + stage + (PL - 1 - c % PL) * L::PLANE) ^ (32 * (c / PL))));
+    };
+    auto value_of = [&](uint32_t stage, int c) { return value_frag(v_at + stage + (PL - 1 - c / NB % PL) * L::PLANE, c / NB / PL, c % NB); };
+    auto key_products = [&](f32x16_t &x, const bf16x8_t &k, int c) {
+#pragma unroll
+        for (int i = TERMS - 1; i >= 0; --i)
+            if (i + PL - 1 - c % PL < PL) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][c / PL], x, 0, 0, 0);
+    };
 
-    if (n_tiles > 0) {
+    // K of tiles 0 and 1 to their stages; zeros where turn 0 looks for the V of a tile before
 #pragma unroll
-        for (int e = 0; e < PIECES; ++e) convert(0, e);
-        if (n_tiles > 1) fetch(1);
-    }
-    for (int t = 0; t < n_tiles; ++t) {
-        // Tile t is in its stage; the other one, which tile t - 1 was read from, takes tile t + 1.
-        wait_lgkm<0>();
-        lds_barrier();
-        const uint32_t now = (t & 1) * L::BYTES, next = L::BYTES - now;
-        if (!mine.has(t)) {
-            if (t + 1 < n_tiles) {
+    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to, e);
+    fetch_k(1);
 #pragma unroll
-                for (int e = 0; e < PIECES; ++e) convert(next, e);
-                if (t + 2 < n_tiles) fetch(t + 2);
-            }
-            continue;
-        }
-        f32x16_t s;
+    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + L::BYTES, e);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
-        // (behind the last tile: what the registers hold goes to a stage that nobody reads)
-        // Fragments are read AHEAD groups of MFMAs before theirs (a wavefront alone on its SIMD waits for what it reads).
-        constexpr int N = PL * KK, AHEAD = 3;
-        bf16x8_t k[AHEAD];
-        auto key_frag = [&](int c) {   // plane PL - 1 - c % PL: small terms first
-            return __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + now + (PL - 1 - c % PL) * L::PLANE) ^ (32 * (c / PL))));
-        };
+    for (int i = 0; i < L::CHUNKS; ++i)
 #pragma unroll
-        for (int c = 0; c < AHEAD; ++c) k[c] = key_frag(c);
+        for (int c = 0; c < PL; ++c) *(lds16)((v_to ^ (128 * i)) + L::BYTES + c * L::PLANE) = u32x4{0, 0, 0, 0};
+    fetch_k(2);
+    wait_lgkm<0>();
+    lds_barrier();
+    f32x16_t s;   // scores of tile t
 #pragma unroll
-        for (int c = 0; c < N; ++c) {
-            const int kk = c / PL, p = PL - 1 - c % PL;
-            __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-            for (int i = TERMS - 1; i >= 0; --i)
-                if (i + p < PL) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[c % AHEAD], q[i][kk], s, 0, 0, 0);
-            if (c + AHEAD < N) k[c % AHEAD] = key_frag(c + AHEAD);
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e)
-                if (e * N / PIECES == c) convert(next, e);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (t + 2 < n_tiles) fetch(t + 2);
-        if (!clear.has(t) | strange) {
-            uint32_t pages = ~0u;
-            if (strange)
-                pages = (known(seq.table[rb.page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[rb.page_at(t, 1)]) ? 0xFFFF0000u : 0u);
-            hide_scores(s, pages >> (4 * half) & seen_bits(a, pos, rb.tile_at(t) * kTileKeys + 4 * half));
-        }
+    for (int c = 0; c < N; ++c) key_products(s, key_frag(0, c), c);
+    hide(s, 0);
+    {
         float top = s[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        top = fmaxf(top, lane_xor(top, 32)) * scale;
-        // a whole number that stays until a score is 2^kSlack beyond it: rescaling is exact, and rare
-        if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
-            const float to = top > m + kSlack ? ceilf(top) : m;
-            const float alpha = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
-            m = to;
-            l *= alpha;
+        raise(top);
+    }
+    for (int t = 0; t <= n_tiles; ++t) {   // (turn n_tiles: the last tile's values)
+        // K of tile t + 1 and V of tile t - 1 are in their stages everywhere, and what is written in this turn has no
+        // readers left: K of tile t + 2 takes tile t's place, V of tile t that of tile t - 2.  (Behind the last tile
+        // what the registers hold goes where nobody reads.)
+        wait_lgkm<0>();
+        lds_barrier();
+        const uint32_t even = (t & 1) * L::BYTES, odd_stage = L::BYTES - even;   // stages of tiles t and t + 2; of t + 1 and t - 1
+        if (!mine.has(t)) {   // (p is 0 then, and s -inf)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + even, e);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+            for (int e = 0; e < PIECES; ++e) convert(raw_v, v_to + even, e);
+            if (t + 1 < n_tiles) fetch(raw_v, block_k[0], hkv * head);
+            fetch_k(t + 3);
+            continue;
         }
-        constexpr int M = 2 * PL * NB;
-        auto value_of = [&](int c) { return value_frag(v_at + now + (PL - 1 - c / NB % PL) * L::PLANE, c / NB / PL, c % NB); };
+        f32x16_t n;   // scores of tile t + 1
+        u32x4 pn[TERMS][2];
+        bf16x8_t f[AHEAD];
         const float ref = m == -INFINITY ? 0.f : m;
-        bf16x8_t p[TERMS][2], v[AHEAD];
-#pragma unroll
-        for (int c = 0; c < AHEAD; ++c) v[c] = value_of(c);
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float w = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -ref));
-            sum += w;
-            __bf16 terms[TERMS];
-            split_terms<TERMS>(w, terms);
+        for (int i = 0; i < 16; ++i) n[i] = 0.f;
+        auto softmax_piece = [&](int e) {   // scores 2 e and 2 e + 1 of tile t
+            const float w0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale, -ref)), w1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale, -ref));
+            sum += w0;
+            sum += w1;
+            uint32_t w[TERMS];
+            cut_terms2<TERMS>(w0, w1, w);
 #pragma unroll
-            for (int j = 0; j < TERMS; ++j) p[j][i / 8][i % 8] = terms[j];
+            for (int j = 0; j < TERMS; ++j) pn[j][e / 4][e % 4] = w[j];
+            asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)
+        };
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c) f[c] = key_frag(odd_stage, c);
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            __builtin_amdgcn_sched_barrier(0);
+            key_products(n, f[c % AHEAD], c);
+            if (c + AHEAD < N) f[c % AHEAD] = key_frag(odd_stage, c + AHEAD);
+            else f[c % AHEAD] = value_of(odd_stage, c + AHEAD - N);
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e)
+                if (e * N / PIECES == c) convert(raw_k, k_to + even, e);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e * N / 4 + 1 == c) softmax_piece(e);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        l += sum;
+        const int b_v = block_k[0];
+        fetch_k(t + 3);
+        if (!clear.has(t + 1) | strange) hide(n, t + 1);
+        float top = -INFINITY;
+        static_assert(N % AHEAD == 0, "the values' first fragments follow the keys' last");
 #pragma unroll
         for (int c = 0; c < M; ++c) {
-            const int pl = PL - 1 - c / NB % PL, h = c / NB / PL, b = c % NB;
+            const int b = c % NB, h = c / NB / PL, pl = PL - 1 - c / NB % PL;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = TERMS - 1; i >= 0; --i)
-                if (i + pl < PL) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c % AHEAD], p[i][h], o[b], 0, 0, 0);
-            if (c + AHEAD < M) v[c % AHEAD] = value_of(c + AHEAD);
+                if (i + pl < PL) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[c % AHEAD], p[i][h], o[b], 0, 0, 0);
+            if (c + AHEAD < M) f[c % AHEAD] = value_of(odd_stage, c + AHEAD);
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e)
+                if (e * M / PIECES == c) convert(raw_v, v_to + even, e);
+#pragma unroll
+            for (int e = 4; e < 8; ++e)
+                if ((e - 4) * M / 4 + 1 == c) softmax_piece(e);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e * M / 8 == c) top = fmaxf(fmaxf(top, n[2 * e]), n[2 * e + 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (t + 1 < n_tiles) fetch(raw_v, b_v, hkv * head);
+        l += sum;
+        s = n;
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) p[i][h] = __builtin_bit_cast(bf16x8_t, pn[i][h]);
+        raise(top);
     }
     auto store = [&] {
         const float sum = l + lane_xor(l, 32);
@@ -276,7 +332,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             load4(k, 16 * kk + 8 * half + 4, STAGE_F32, y + 4);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                bad |= !(fabsf(y[j]) <= kLargest);
+                bad |= !(fabsf(y[j]) < INFINITY);
                 w = fmaf(x[j], y[j], w);
             }
             asm volatile("" ::: "memory");   // (registers)
@@ -296,7 +352,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
                 load4(v, 32 * c + 8 * j + 4 * half, STAGE_F32, x);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    bad |= !(fabsf(x[e]) <= kLargest);
+                    bad |= !(fabsf(x[e]) < INFINITY);
                     o[c][4 * j + e] = o[c][4 * j + e] * alpha + (seen ? w * x[e] : 0.f);
                 }
                 __builtin_amdgcn_sched_barrier(0);   // (registers)

@@ -97,6 +97,24 @@ __device__ __forceinline__ void split_terms(float x, __bf16 t[TERMS]) {
     }
 }
 
+// Two numbers (a in the low halves) at once.  One term is the nearest bf16; several are cut from the bits, each the leading
+// 8 of what the ones before leave, so three hold all 24 as well, in fewer instructions than by rounding.
+template <int TERMS>
+__device__ __forceinline__ void cut_terms2(float a, float b, uint32_t t[TERMS]) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (TERMS == 1) {
+        t[0] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    } else {
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) {
+            t[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+            if (i == TERMS - 1) break;
+            a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+            b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+        }
+    }
+}
+
 // Bits 0 .. n of a word.
 __device__ __forceinline__ uint32_t bits_to(int n) { return n < 0 ? 0u : ~0u >> (31 - min(n, 31)); }
 // sees(), for the 32 keys from k0 on.
