@@ -432,12 +432,23 @@ SplitPlan split_plan(const WindowArgs &a) {
     const long listed = (a.sinks + kPage - 1) / kPage + ((long)a.window + bq + 2 * kPage - 3) / kPage;
     const long pages = listed < all ? listed : all;
     const long blocks = (long)a.rows.n_seqs * p.blocks_per_seq * a.n_kv_heads;
-    const long groups = 2L * device_compute_units();
-    const long splits = blocks >= groups ? 1 : (groups + blocks - 1) / blocks;
-    // (four pages a wavefront at least: the joining launch costs more than those take)
-    p.pages = (int)((pages + 4 * splits - 1) / (4 * splits));
-    p.pages = p.pages < 4 ? 4 : p.pages;
-    p.splits = (int)((pages + 4L * p.pages - 1) / (4L * p.pages));
+    // Workgroups that run at once: 128 KB of LDS each, 64 KB with bf16 heads of 64.  As many splits as fill one to four
+    // rounds of them, whichever ends first: a round takes a wavefront's pages and the time of three to begin and end, the
+    // joining launch as much (16 rows over 1024 fp32 tokens in two rounds 43 us, in one 38; 20 rows over 4096 bf16 tokens, 64
+    // heads, in two rounds 80, in one of twice the length 90).  Four pages a wavefront at least.
+    const long units = (a.head_dim == 64 && a.kv_type == STAGE_BF16 ? 2L : 1L) * device_compute_units();
+    long least = 0;
+    for (long rounds = 0; rounds <= 4; ++rounds) {
+        const long want = rounds * units / (blocks > 0 ? blocks : 1), s = want < 1 ? 1 : want;
+        long n = (pages + 4 * s - 1) / (4 * s);
+        n = n < 4 ? 4 : n;
+        const long splits = pages <= 4 * n ? 1 : (pages + 4 * n - 1) / (4 * n);
+        const long cost = (blocks * splits + units - 1) / units * (n + 3) + (splits > 1 ? 3 : 0);
+        if (rounds > 0 && cost >= least) continue;
+        least = cost;
+        p.pages = (int)n;
+        p.splits = (int)splits;
+    }
     return p;
 }
 
