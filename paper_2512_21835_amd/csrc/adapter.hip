@@ -97,7 +97,7 @@ struct AdapterPlan {
 
 // t of a tile over a slice of k: a wavefront holds its k of x as operand fragments and takes one item (adapter, 16 of its
 // ranks) after the other, its rows of A copied into LDS one item ahead; the four wavefronts' sums meet in LDS.
-constexpr int kWaveK = 256;
+constexpr int kWaveK = 128;
 template <int TERMS>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, AdapterPlan pl) {
     constexpr int TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32, STEPS = kWaveK / kStep, CH = kWaveK / 8;
@@ -248,8 +248,9 @@ __device__ __forceinline__ void wait_most(int n) {
 // A workgroup: a tile and blocks of 64 columns of out, a wavefront each.  A block's items are the tile's adapters, and
 // of each up to 64 ranks at a time; B's of the next item (and base's of a block with its first) are copied into LDS
 // while one is multiplied; the loop has no load of another kind, whose wait would take in the copies.  WAYS
-// wavefronts share the blocks, each with every WAYS-th adapter, whose rows it writes (the first also those without
-// one).  A lane has 16 neighbouring columns of a row: MFMA m's row i is column 16 (i / 4) + 4 m + i % 4 of the block.
+// wavefronts share the blocks, and so may workgroups (grid z), each with every so manieth adapter, whose rows it writes (the
+// first also those without one): 16 rows of 16 adapters, 64 blocks, 4 workgroups to a block take
+// 6.6 us, one 9.6.  A lane has 16 neighbouring columns of a row: MFMA m's row i is column 16 (i / 4) + 4 m + i % 4 of the block.
 //
 // A turn is as long as the latency of its own instructions, of one or two wavefronts per SIMD, so it has few: the items,
 // the same for every block, are listed once, an item per lane; t's fragments stay in registers.
@@ -272,12 +273,12 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
     t.load(a, row0);
     // this wavefront's items, an item per lane: B's first place for it, how many of the adapter's ranks are left, and
     // the adapter; and whether the lane's row is its to write
-    const int way = wave % WAYS;
+    const int way = wave % WAYS + WAYS * blockIdx.z, ways = WAYS * gridDim.z;
     const uint16_t *item_b = nullptr;
     int item_ranks = 0, item_id = -1, n_items = 0, seen = 0;
     bool write = t.id < 0 && way == 0;
     for (unsigned left = t.first; left; left &= left - 1, ++seen)
-        if (seen % WAYS == way) {
+        if (seen % ways == way) {
             const int at = __builtin_ctz(left), id = __builtin_amdgcn_readlane(t.id, at), rank = __builtin_amdgcn_readlane(t.rank, at);
             const int mine = lane - n_items;
             if (mine >= 0 && kRanks * mine < rank) {
@@ -289,9 +290,10 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterP
             write |= t.id == id;
         }
     write &= row < a.rows;
-    if (n_items == 0) n_items = 1;   // (of no rank: base to out)
     const bool any = __builtin_amdgcn_ballot_w64(write) != 0, wide = R % 8 == 0;
-    const int n_blocks = (a.n + kCols - 1) / kCols, end = min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
+    const int n_blocks = (a.n + kCols - 1) / kCols;
+    const int end = blockIdx.z > 0 && !any ? 0 : min(n_blocks, (int)(blockIdx.x + 1) * blocks_per_group);
+    if (n_items == 0) n_items = 1;   // (of no rank: base to out)
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * L::bytes(R);
     const uint32_t y_ring = ring + S * b_stage;
 
@@ -532,7 +534,9 @@ hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles,
     const int least = shared ? 1 : 4;
     long per = ((long)blocks * tiles + want - 1) / want;
     per = (per + least - 1) / least * least;
-    const dim3 grid((unsigned)((blocks + per - 1) / per), tiles);
+    // fewer workgroups than run at once: more of them share a block's adapters, four of which each takes
+    const long most = ((a.n_adapters < kTile ? a.n_adapters : kTile) + 3) / 4, room = want / ((long)blocks * tiles);
+    const dim3 grid((unsigned)((blocks + per - 1) / per), tiles, (unsigned)(!shared || room < 2 ? 1 : room < most ? room : most));
     auto launch = [&](auto ways, auto steps) -> hipError_t {
         auto *const kernel = adapter_up_kernel<TYPE, decltype(ways)::value, decltype(steps)::value>;
         STG_LAUNCH(kernel, grid, dim3(256), lds, st, a, p, (int)per);
