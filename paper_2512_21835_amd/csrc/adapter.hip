@@ -262,7 +262,7 @@ struct UpLds {   // a wavefront's: S stages of B (by the adapters' rank), S of b
     static constexpr int bytes(int max_rank) { return S * (b_stage(max_rank) + Y_STAGE); }
 };
 template <int TYPE, int WAYS, int T_STEPS>
-__global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, AdapterPlan pl, int blocks_per_group) {
+__global__ __launch_bounds__(256, T_STEPS * kStep <= kRanks ? 3 : 1) void adapter_up_kernel(AdapterArgs a, AdapterPlan pl, int blocks_per_group) {
     using L = UpLds<TYPE>;
     constexpr int S = L::S, E = L::E, YCOPIES = L::YCOPIES, YCH = kCols * E / 16;
     extern __shared__ __align__(1024) char lds[];
@@ -528,7 +528,8 @@ AdapterPlan adapter_plan(const AdapterArgs &a) {
 template <int TYPE>
 hipError_t launch_up(const AdapterArgs &a, const AdapterPlan &p, unsigned tiles, hipStream_t st) {
     const int blocks = (a.n + kCols - 1) / kCols, lds = 4 * UpLds<TYPE>::bytes(a.max_rank);
-    const long want = (lds > 80 * 1024 ? 1L : 2L) * device_compute_units();   // workgroups: as many as run at once
+    // workgroups: as many as run at once (by LDS; the registers are held to those of three, 4001 rows of rank 32 58 -> 52 us)
+    const long want = (lds > 80 * 1024 ? 1L : lds > 53 * 1024 ? 2L : 3L) * device_compute_units();
     // few tiles: the wavefronts share a block's adapters; many: a block each
     const bool shared = p.groups > 1 && a.n_adapters >= 4;
     const int least = shared ? 1 : 4;
