@@ -9,6 +9,10 @@
 // Every operand goes through LDS, with neighbouring lanes side by side in memory (weights by copies straight into a
 // ring of each wavefront's own): an MFMA operand read straight from memory has neighbouring lanes in different rows,
 // 55 cache accesses per instruction, which alone took 30 of the up kernel's 53 us at 64 rows of a 70B-shaped projection.
+//
+// Down and up: 16 rows of 16 adapters of rank 16, 4096 x 4096, fp32, 5.6 + 6.6 us (latency of the launches); 64 bf16 rows of
+// 48 adapters up to rank 64, 8192 x 28672 (135 MB), 9 + 32 us (the up kernel 4 TB/s); 4001 bf16 rows of 3 adapters of rank
+// 32, 5120 x 5120 (125 MB), 16.6 + 26 us (3.2 TB/s: a block's base is copied one block ahead only).
 #include <type_traits>
 
 #include "lanes.h"

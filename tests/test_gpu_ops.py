@@ -183,6 +183,15 @@ def test_window_prompts_of_many_heads(hq, hkv, d, cache, act):
         _check_window(c, _run_window(c, window, sinks), window, sinks)
 
 
+@pytest.mark.parametrize("last,hq,hkv", [(50, 4, 2), (5, 1, 1), (900, 8, 1)])    # (the last: whole tiles)
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+def test_window_more_sequences_than_a_wavefront_has_lanes(cache, last, hq, hkv):
+    rows = [1, 0, 3] * 30 + [last] + [2] * 9
+    c = _window_case(rows, [7 * i % 90 for i in range(len(rows))], hq, hkv, 64, "fp32", cache, pad=2)
+    for window, sinks in ((0, 0), (30, 5)):
+        _check_window(c, _run_window(c, window, sinks), window, sinks)
+
+
 @pytest.mark.parametrize("hkv", [1, 8])
 @pytest.mark.parametrize("cache", ["bf16", "fp32"])
 def test_window_long_prompt_and_long_cache(cache, hkv):
