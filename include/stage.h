@@ -227,7 +227,7 @@ int stage_set_adapter(stage *s, int32_t mb, int32_t b, int32_t id);
    and run for all rows of the call before their slot is reused (Section III-A: loading
    overlapped with computation of other layers; the bursty pattern serves several micro-batches
    per load).  KV blocks are taken in call order (mb_ids order, then b ascending).
-   EINVAL: bad ids/sizes or a layer not loaded; ERANGE: a sequence would exceed max_context;
+   EINVAL: bad ids/sizes, a layer not loaded, or more than STAGE_OPS_MAX_ROWS rows with head_norm, a window or adapters; ERANGE: a sequence would exceed max_context;
    ENOMEM: KV pool exhausted. */
 int stage_prefill(stage *s, int32_t n_mb, const int32_t *mb_ids, int32_t B, int32_t T,
                   const float *x_in, float *x_out);

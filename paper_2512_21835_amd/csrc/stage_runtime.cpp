@@ -623,8 +623,8 @@ WindowArgs window_args(const stage *s, int layer, int rows, int T, const RowMap 
     w.n_q_heads = s->Hq;
     w.n_kv_heads = s->Hkv;
     w.head_dim = s->D;
-    w.window = s->cfg.window;
-    w.sinks = s->cfg.sinks;
+    w.window = std::min(s->cfg.window, s->cfg.max_context);   // (the kernels subtract it from positions)
+    w.sinks = std::min(s->cfg.sinks, s->cfg.max_context);
     w.scale = 1.f / std::sqrt((float)s->D);
     w.rows = op_rows(s, rows, T, meta);
     return w;
@@ -1387,6 +1387,9 @@ int run_call_body(stage *s, int n_mb, const int32_t *mb_ids, int B, int T, const
     }
     for (int l = 0; l < s->L; ++l)
         if (!s->layers[l].loaded) return s->fail(STAGE_EINVAL, "layer %d is not loaded", l);
+    if (has_ops(s) && (long)slots.size() * T > STAGE_OPS_MAX_ROWS)
+        return s->fail(STAGE_EINVAL, "%ld rows in a call (with head_norm, a window or adapters at most %d)", (long)slots.size() * T,
+                       STAGE_OPS_MAX_ROWS);
     int longest = 0;
     for (int len : s->lengths) longest = std::max(longest, len);
     int need_blocks = 0, max_ctx = 0;

@@ -451,7 +451,7 @@ SplitPlan split_plan(const WindowArgs &a) {
     const long seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
     const long equal = (long)a.rows.n_seqs * ((most + bq - 1) / bq), ragged = a.rows.rows / bq + seqs;
     const long blocks = (p.one_block || equal < ragged ? equal : ragged) * a.n_kv_heads;
-    p.blocks = blocks > 0x7FFFFFFF ? 0 : (int)blocks;
+    p.blocks = blocks > kMaxBlocks ? 0 : (int)blocks;
     // Workgroups that run at once: 128 KB of LDS each, 64 KB with bf16 heads of 64.  As many splits as fill one to four
     // rounds of them, whichever ends first: a round takes a wavefront's pages and the time of three to begin and end, the
     // joining launch as much (16 rows over 1024 fp32 tokens in two rounds 43 us, in one 38; 20 rows over 4096 bf16 tokens, 64
@@ -626,7 +626,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
             for (int i = 0; i < L::COPIES; ++i) {
                 u32x4 v = *(lds16)(at + 1024 * i);
                 const bool bad = clear_odd(v);
-                odd |= bad;
+                odd |= bad & rb.sees(a, rb.tile_at(t) * KT + 8 * wave + lane / L::CH + L::KPC * i);
                 if (bad) *(lds16)(at + 1024 * i) = v;
             }
         }
@@ -870,7 +870,7 @@ hipError_t launch_tiles(const WindowArgs &a, hipStream_t st) {
     // row blocks: no sequence adds more than one that is not full
     const int bq = 128 >> p.log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
     const long blocks = ((long)a.rows.rows / bq + seqs) * a.n_kv_heads;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (blocks > kMaxBlocks) return hipErrorInvalidValue;
     STG_LAUNCH((window_tiles<D, TERMS>), dim3((unsigned)blocks), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }

@@ -77,21 +77,21 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         block_k[1] = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
         fetch(raw_k, block_k[1], 0);
     };
-    // A K or V that is not finite becomes 0: the columns that see it are taken again at the end.
-    bool odd = false;
+    // A K or V that is not finite becomes 0: the columns that see it, if any does, are taken again at the end.
+    bool odd = false, bad_k = false, bad_v = false;
     const int my_key = 8 * wave + lane / 8;
     const uint32_t k_to = base + my_key * L::ROW + 16 * (lane % 8 ^ L::kx(my_key));
     const uint32_t v_to = base + L::HALF + my_key * L::ROW + 16 * (lane % 8 ^ L::vx(my_key));
     u32x4 planes[PL];
     constexpr int PIECES = 4 * L::CHUNKS;   // two elements each
-    auto convert = [&](const f32x4_t(&raw)[L::CHUNKS][2], uint32_t to, int piece) {
+    auto convert = [&](const f32x4_t(&raw)[L::CHUNKS][2], uint32_t to, int piece, bool &any_bad) {
         const int i = piece / 4, e0 = piece % 4 * 2;
         float x[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             x[e] = raw[i][e0 / 4][e0 % 4 + e];
             const bool bad = !(fabsf(x[e]) < INFINITY);
-            odd |= bad;
+            any_bad |= bad;
             x[e] = bad ? 0.f : x[e];
         }
         uint32_t w[PL];
@@ -102,6 +102,13 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
 #pragma unroll
             for (int p = 0; p < PL; ++p) *(lds16)((to ^ (128 * i)) + p * L::PLANE) = planes[p];
         }
+    };
+
+    // Whether the thread's key of tile t was bad, if that is a tile and some row sees the key.
+    auto noted = [&](bool &bad, int t) {
+        if (__builtin_amdgcn_ballot_w64(bad) == 0) return;
+        odd |= bad & (t < n_tiles) & rb.sees(a, rb.tile_at(t) * kTileKeys + my_key);
+        bad = false;
     };
 
     // the wavefront's columns and the rows that they have: positions w_first .. w_last
@@ -189,10 +196,12 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
 
     // K of tiles 0 and 1 to their stages; zeros where turn 0 looks for the V of a tile before
 #pragma unroll
-    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to, e);
+    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to, e, bad_k);
+    noted(bad_k, 0);
     fetch_k(1);
 #pragma unroll
-    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + L::BYTES, e);
+    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + L::BYTES, e, bad_k);
+    noted(bad_k, 1);
 #pragma unroll
     for (int i = 0; i < L::CHUNKS; ++i)
 #pragma unroll
@@ -221,9 +230,11 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         const uint32_t even = (t & 1) * L::BYTES, odd_stage = L::BYTES - even;   // stages of tiles t and t + 2; of t + 1 and t - 1
         if (!mine.has(t)) {   // (p is 0 then, and s -inf)
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + even, e);
+            for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + even, e, bad_k);
+            noted(bad_k, t + 2);
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) convert(raw_v, v_to + even, e);
+            for (int e = 0; e < PIECES; ++e) convert(raw_v, v_to + even, e, bad_v);
+            noted(bad_v, t);
             if (t + 1 < n_tiles) fetch(raw_v, block_k[0], hkv * head);
             fetch_k(t + 3);
             continue;
@@ -255,12 +266,13 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             else f[c % AHEAD] = value_of(odd_stage, c + AHEAD - N);
 #pragma unroll
             for (int e = 0; e < PIECES; ++e)
-                if (e * N / PIECES == c) convert(raw_k, k_to + even, e);
+                if (e * N / PIECES == c) convert(raw_k, k_to + even, e, bad_k);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e * N / 4 + 1 == c) softmax_piece(e);
             __builtin_amdgcn_sched_barrier(0);
         }
+        noted(bad_k, t + 2);
         const int b_v = block_k[0];
         fetch_k(t + 3);
         if (!clear.has(t + 1) | strange) hide(n, t + 1);
@@ -276,7 +288,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             if (c + AHEAD < M) f[c % AHEAD] = value_of(odd_stage, c + AHEAD);
 #pragma unroll
             for (int e = 0; e < PIECES; ++e)
-                if (e * M / PIECES == c) convert(raw_v, v_to + even, e);
+                if (e * M / PIECES == c) convert(raw_v, v_to + even, e, bad_v);
 #pragma unroll
             for (int e = 4; e < 8; ++e)
                 if ((e - 4) * M / 4 + 1 == c) softmax_piece(e);
@@ -285,6 +297,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
                 if (e * M / 8 == c) top = fmaxf(fmaxf(top, n[2 * e]), n[2 * e + 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        noted(bad_v, t);
         if (t + 1 < n_tiles) fetch(raw_v, b_v, hkv * head);
         l += sum;
         s = n;
@@ -375,7 +388,7 @@ hipError_t launch(const WindowArgs &a, hipStream_t st) {
     // row blocks: no sequence adds more than one that is not full
     const int bq = 128 >> log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
     const long blocks = ((long)a.rows.rows / bq + seqs) * a.n_kv_heads;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (blocks > kMaxBlocks) return hipErrorInvalidValue;
     STG_LAUNCH((window_tiles_f32<D, TERMS, PL>), dim3((unsigned)blocks), dim3(256), 0, st, a, log_g);
     return hipGetLastError();
 }

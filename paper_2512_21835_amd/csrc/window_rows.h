@@ -24,6 +24,7 @@ typedef __attribute__((address_space(3))) s16x4_t *lds8;
 typedef __attribute__((address_space(3))) float *lds4;
 
 constexpr int kPage = kBlockTokens;
+constexpr long kMaxBlocks = (1L << 24) - 1;   // workgroups of 256 in a grid: their threads are counted in 32 bits
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;
 
@@ -171,6 +172,10 @@ struct RowBlock {
         from = max(max(0, first - a.window + 1) / kTileKeys, sink);
         n_tiles = end <= 0 ? 0 : sink + max(0, (end + kTileKeys - 1) / kTileKeys - from);
         return true;
+    }
+    // whether some row sees the key
+    __device__ __forceinline__ bool sees(const WindowArgs &a, int key) const {
+        return (key < end) & ((key > first - a.window) | (key < a.sinks));
     }
     __device__ __forceinline__ int tile_at(int t) const { return t < sink ? t : from + t - sink; }
     // page h of tile t, of those that hold a key of the sequence

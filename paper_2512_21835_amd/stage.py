@@ -220,7 +220,7 @@ def stage_load_layer(h, layer: int, weights: Optional[Dict[str, object]], reside
         _check(lib().stage_load_layer(h, layer, None, int(resident)), h)
         return
     w = StageLayerWeights(*[_ptr(weights[n]) for n in ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2")],
-                          *[_ptr(weights[n]) for n in ("gq", "gk") if n in weights])
+                          **{n: _ptr(weights[n]) for n in ("gq", "gk") if n in weights})
     _check(lib().stage_load_layer(h, layer, ctypes.byref(w), int(resident)), h)
 
 

@@ -212,6 +212,28 @@ def test_a_captured_decode_replayed():
             P.stage_destroy(h)
 
 
+def test_a_window_beyond_every_sequence_is_none():
+    big = (1 << 31) - 1
+    plain, wide = Model(SHAPES[64], head_norm=True), Model(SHAPES[64], head_norm=True, window=big, sinks=big)
+    xs, outs = _run(wide, 3, 40)
+    _check(outs, _want(plain, 3, xs))
+
+
+def test_more_rows_than_the_operators_take_are_refused():
+    s = dataclasses.replace(SHAPES[64], n_layers=1)
+    m = Model(s, head_norm=True)
+    h = P.stage_init(m.config(max_microbatches=1, max_batch=64, max_context=16384, kv_pool_blocks=64))
+    try:
+        m.load(h)
+        x = torch.zeros(1, 1, 256, device="cuda")       # (not read)
+        with pytest.raises(P.StageError) as e:           # 2^20 rows
+            P.stage_prefill(h, [0], 64, 16384, x, x.clone())
+        assert e.value.code == P.STAGE_EINVAL
+        assert P.stage_get_length(h, 0, 0) == 0
+    finally:
+        P.stage_destroy(h)
+
+
 def test_adapters_come_and_go():
     m = Model(SHAPES[64], adapters=True)
     with harness.compute_stream() as cs:
