@@ -54,12 +54,12 @@ __device__ __forceinline__ void load_f32x8(const float *p, float v[8]) {
 template <int SP, int D>
 __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     constexpr int HALF = D / 2, TPH = D / 16;
-    const int lrow = blockIdx.x, row = a.row0 + lrow;
+    const int row = blockIdx.x;
     const int hq = a.n_q_heads, hkv = a.n_kv_heads, heads = hq + 2 * hkv;
     const int t = blockIdx.y * 256 + threadIdx.x, j = 8 * (t % TPH);
     const int h = min(t / TPH, heads - 1);
     float x1[8], x2[8];
-    const size_t e = (size_t)lrow * a.qkv_ld + (size_t)h * D + j;
+    const size_t e = (size_t)row * a.qkv_ld + (size_t)h * D + j;
     load_row8<SP>(a, e, x1);
     load_row8<SP>(a, e + HALF, x2);
 
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
         }
     }
     if (h < hq) {
-        const size_t o = (size_t)lrow * a.q_ld + (size_t)h * D + j;
+        const size_t o = (size_t)row * a.q_ld + (size_t)h * D + j;
         store8(a.q_out, o, a.q_type, x1);
         store8(a.q_out, o + HALF, a.q_type, x2);
     } else {   // head h - hq of K then V
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
 template <int D>
 hipError_t launch_d(const AppendArgs &a, hipStream_t st) {
     const int threads = (a.n_q_heads + 2 * a.n_kv_heads) * (D / 16);
-    const dim3 grid(a.n_rows, (threads + 255) / 256);
+    const dim3 grid(a.rows.rows, (threads + 255) / 256);
     switch (a.qkv_type == STAGE_BF16 ? 0 : a.n_part) {
 #define STG_APPEND_CASE(SP) \
     case SP: STG_LAUNCH((norm_rope_append_kernel<SP, D>), grid, dim3(256), 0, st, a); break;
@@ -147,7 +147,7 @@ hipError_t launch_d(const AppendArgs &a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_norm_rope_append(const AppendArgs &a, hipStream_t st) {
-    if (a.n_rows <= 0) return hipSuccess;
+    if (a.rows.rows <= 0) return hipSuccess;
     return a.head_dim == 64 ? launch_d<64>(a, st) : a.head_dim == 128 ? launch_d<128>(a, st) : hipErrorInvalidValue;
 }
 

@@ -178,7 +178,6 @@ int stage_norm_rope_append(const stage_append_args *p, void *stream) {
     r.n_kv_heads = a.cache.n_kv_heads;
     r.head_dim = d;
     r.kv_type = a.cache.type;
-    r.n_rows = a.rows;
     r.rows = op_rows(a.batch, a.cache, a.rows);
     DeviceGuard dg(a.device);
     return status(launch_norm_rope_append(r, static_cast<hipStream_t>(stream)));

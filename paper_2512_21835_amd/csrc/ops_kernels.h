@@ -65,7 +65,6 @@ struct AppendArgs {
     int axis1, axis2;          // first pairs of the second and third axis (head_dim / 2: none)
     void *pool;
     int n_q_heads, n_kv_heads, head_dim, kv_type;
-    int row0, n_rows;          // rows of this launch: row0 .. row0 + n_rows - 1 of the call's (qkv, q_out: of row0)
     OpRows rows;
 };
 hipError_t launch_norm_rope_append(const AppendArgs &a, hipStream_t st);

@@ -969,7 +969,6 @@ int run_append(stage *s, int layer, const LayerWeights &w, int rows, int T, cons
     a.n_kv_heads = s->Hkv;
     a.head_dim = s->D;
     a.kv_type = kv.kv_type;
-    a.n_rows = rows;
     a.rows = op_rows(s, rows, T, meta);
     HIP_TRY(launch_norm_rope_append(a, s->cs));
     return STAGE_OK;

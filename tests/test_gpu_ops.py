@@ -286,6 +286,36 @@ def test_window_strides_stream_and_given_workspace():
             P.stage_window_attention(wide_q[:, 1:9], wide_o[:, 3:11], pool, batch, window=2000, sinks=4, workspace=ws[:need - 16])
 
 
+@pytest.mark.parametrize("act,cache", [("bf16", "bf16"), ("fp32", "bf16"), ("fp32", "fp32"), ("bf16", "fp32")])
+@pytest.mark.parametrize("rows,hkv", [([30, 5], 52), ([30, 5], 2)])     # (whole tiles, and 16 columns at a time)
+def test_window_prompts_strided_on_a_stream_and_captured(rows, hkv, act, cache):
+    b, q, out = c = _window_case(rows, [70, 3], 4 * hkv, hkv, 64, act, cache)
+    want = _run_window(c, 40, 2)
+    wide_q, wide_o = (torch.zeros(35, 4 * hkv + 3, 64, dtype=q.dtype, device=DEV) for _ in range(2))
+    wide_q[:, 1:-2] = q.to(DEV)
+    pool, batch = b.pool.to(DEV), b.stage_batch(P)
+    need = P.stage_window_workspace(wide_q[:, 1:-2], wide_o[:, 2:-1], pool, batch, 40, 2)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device=DEV)
+
+    def call(stream):
+        P.stage_window_attention(wide_q[:, 1:-2], wide_o[:, 2:-1], pool, batch, window=40, sinks=2, workspace=ws, stream=stream)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    call(stream)
+    stream.synchronize()
+    assert torch.equal(wide_o[:, 2:-1], want) and not bool(wide_o[:, :2].any()) and not bool(wide_o[:, -1].any())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call(stream)
+    for _ in range(3):
+        wide_o.zero_()
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(wide_o[:, 2:-1], want)
+
+
 # ------------------------------------------------------------------------------------------------ adapters
 
 def _adapter_case(rows, k, n, adapters, rank, act, ids, ranks=None, scales=True, seed=3):

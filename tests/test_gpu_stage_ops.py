@@ -152,6 +152,12 @@ def test_stage(what, shape, B, T):
     assert what == "window" and T < WINDOW or harness.fp32_errors(plain[1], want[1])[0] > 20 * harness.FP32_REL
 
 
+def test_stage_of_more_rows_than_k_is_cut_for():
+    m = Model(dataclasses.replace(SHAPES[64], n_layers=1), **FEATURES["all"])
+    xs, outs = _run(m, 24, 46, steps=1)
+    _check(outs, _want(m, 24, xs))
+
+
 def test_stage_with_a_bf16_cache():
     """K and V may be a rounding step off where fp32 and float64 fall on either side of a boundary: at most 2^-8 of
     each, so 2^-8 of what the values add up to, and as much again of scores of size 1 or so through the keys."""
