@@ -18,7 +18,7 @@ namespace {
 // (2^-9 of a probability, as everywhere with bf16 rows) and two planes, 2^-16, are well below that.
 //
 // In turn t: K of tile t + 1 by Q, then V of tile t - 1 by P, and between their MFMAs the softmax of tile t, the terms of
-// K of tile t + 2 and of V of tile t.  2 x 600 fp32 rows of 40 heads behind 300 tokens, window 256: 105 us, 0.6 PFLOP/s
+// K of tile t + 2 and of V of tile t.  2 x 600 fp32 rows of 40 heads behind 300 tokens, window 256: 106 us, 0.6 PFLOP/s
 // issued over whole tiles.  A turn takes 3.2 us, 1.6 of them MFMAs, alone on its SIMD (three terms of q, 96 registers, leave
 // no room for a second wavefront), and 400 workgroups are two rounds of 256.  Without the overlap 111 us; 16 columns at a
 // time with fp32 MFMAs (window_split) 262 us.
