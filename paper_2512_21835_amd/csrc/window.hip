@@ -7,7 +7,7 @@
 // window_split: rows in blocks of 16 columns (G query heads of a KV head x 16 / G positions), the pages cut
 // over workgroups and their wavefronts, states joined at the end (window_merge where the workgroups are several).
 // Bound by the cache's bytes: 64 single tokens of 64 heads over up to 4096 bf16 tokens each (8 KV heads, 727 MB)
-// 132 us, 5.5 TB/s; a page costs a wavefront 1.2 us of dependent reads, products and softmax (fp32: 2.3), which
+// 140 us, 5.2 TB/s; a page costs a wavefront 1.2 us of dependent reads, products and softmax (fp32: 2.3), which
 // is what shorter lists take (16 tokens of 32 heads over up to 1024 fp32 tokens, 83 MB: 38 us).
 //
 // window_tiles: prompts over a bf16 cache (over an fp32 cache: window_f32.hip).
@@ -56,11 +56,12 @@ struct PageLds {
 //
 // S^T = K Q^T: lane l holds keys 4 (l / 16) + i of the page for column l % 16, which is the layout of the operand P^T of
 // O^T += V^T P^T, so probabilities stay in registers; o[b][i]: d 16 b + 4 (l / 16) + i of column l % 16.  bf16 cache:
-// 16x16x32 and 16x16x16 MFMAs, V^T by transposing reads, q and p as TERMS bf16 terms.  fp32 cache: 16x16x4 fp32 MFMAs, k
+// 16x16x32 and 16x16x16 MFMAs, V^T by transposing reads, q as TERMS bf16 terms and p as p_terms().  fp32 cache: 16x16x4 fp32 MFMAs, k
 // index l / 16 of step (v, c) being d 16 v + 4 (l / 16) + c, so that K is read 16 bytes at a time.
 template <int D, bool F32, int TERMS>
 struct Columns {
     using L = PageLds<D, F32>;
+    static constexpr int PT = p_terms(TERMS);
     bf16x8_t q[F32 ? 1 : TERMS][D / 32];
     float qf[F32 ? D / 4 : 1];
     f32x4_t o[D / 16];
@@ -178,13 +179,13 @@ struct Columns {
 #pragma unroll
                 for (int b = 0; b < D / 16; ++b) o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][b], p[i], o[b], 0, 0, 0);
         } else {
-            s16x4_t pt[TERMS];
+            s16x4_t pt[PT];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                __bf16 t[TERMS];
-                split_terms<TERMS>(p[i], t);
+                __bf16 t[PT];
+                split_terms<PT>(p[i], t);
 #pragma unroll
-                for (int j = 0; j < TERMS; ++j) pt[j][i] = __builtin_bit_cast(short, t[j]);
+                for (int j = 0; j < PT; ++j) pt[j][i] = __builtin_bit_cast(short, t[j]);
             }
             // a transposing read gives 16 lanes the 4 keys x 16 d that they point at (lane i: key i / 4, d 4 (i % 4) ..
             // + 3) column-wise: lane i all keys of d i
@@ -198,7 +199,7 @@ struct Columns {
 #pragma unroll
             for (int b = 0; b < D / 16; ++b)
 #pragma unroll
-                for (int j = 0; j < TERMS; ++j) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[b], pt[j], o[b], 0, 0, 0);
+                for (int j = 0; j < PT; ++j) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[b], pt[j], o[b], 0, 0, 0);
         }
     }
 
@@ -487,16 +488,17 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
 // Prompts.  A workgroup: 128 columns = G heads x BQ = 128 / G consecutive rows of one sequence, one KV head; wavefront
 // w the columns 32 w .. (column r: head r / BQ, row r % BQ).  K and V tiles of 32 keys (two pages) go straight into
 // a ring of LDS stages, one barrier per tile.  S^T = K Q^T: lane l holds keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for
-// column l % 32, the k order of the operand P^T of O^T += V^T P^T; 32x32x16 MFMAs, q and p as TERMS bf16 terms.
+// column l % 32, the k order of the operand P^T of O^T += V^T P^T; 32x32x16 MFMAs, q as TERMS bf16 terms, p as p_terms().
 //
 // In turn t a wavefront multiplies tile t + 1's K by Q and then tile t - 1's V by P while it takes the softmax of
 // tile t: the three are independent, and the vector instructions of the softmax (as long as the MFMAs with one
-// term) are laid between the MFMAs by hand.  Fragments are in registers half a turn before their MFMAs: V's are
+// term of q) are laid between the MFMAs by hand.  Fragments are in registers half a turn before their MFMAs: V's are
 // read under the scores, K's of the tile behind under the values.
 //
-// 4 x 2048 bf16 rows of 64 heads, window 1024: 285 us, 0.73 PFLOP/s; a loop turn runs at 0.88, the rest is beginning
-// (block search, page ids, first tiles: 3 to 4 us a workgroup), end, and the halves of tiles outside the window.  256
-// columns a workgroup (each wavefront 64) take 385 us: one wavefront per SIMD hides less than two.  fp32 rows issue three
+// 4 x 2048 bf16 rows of 64 heads, window 1024: 359 us, 0.86 PFLOP/s of issued products (1.5 times the formula's, for the
+// probabilities' second term; with one term, the output off by its own rounding once more, 286 us).  What is not loop is
+// beginning (block search, page ids, first tiles: 3 to 4 us a workgroup), end, and the halves of tiles outside the window.
+// 256 columns a workgroup (each wavefront 64) are slower: one wavefront per SIMD hides less than two.  fp32 rows issue three
 // times the products: 12 prompts of up to 500 rows, window 512, 122 us.
 template <int D>
 struct TileLds {
@@ -527,7 +529,7 @@ struct TilePlan {
 template <int D, int TERMS>
 __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowArgs a, TilePlan pl) {
     using L = TileLds<D>;
-    constexpr int S = L::STAGES, KK = D / 16, NB = D / 32, KT = L::KEYS;
+    constexpr int S = L::STAGES, KK = D / 16, NB = D / 32, KT = L::KEYS, PT = p_terms(TERMS);
     constexpr int TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32;   // of q and out
     __shared__ __align__(1024) char lds[S * L::BYTES];
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -647,7 +649,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
     // The maximum that scores are taken relative to: a whole number (so that rescaling is exact, what is already
     // rounded to bf16 included) which stays until a score is 2^kSlack beyond it: p and its sums are floating
     // point, and the rescaling, a quarter of a tile's vector work, is rare after the first tile.
-    auto raise = [&](float top, bf16x8_t(&p)[TERMS][2]) {
+    auto raise = [&](float top, bf16x8_t(&p)[PT][2]) {
         const float best = fmaxf(top, lane_xor(top, 32)) * scale;
         if (__builtin_amdgcn_ballot_w64(best > m + kSlack) == 0) return;
         const float to = best > m + kSlack ? ceilf(best) : m;
@@ -659,7 +661,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
 #pragma unroll
-        for (int i = 0; i < TERMS; ++i)
+        for (int i = 0; i < PT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -667,12 +669,12 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
     };
 
     f32x16_t s;               // scores of tile t
-    bf16x8_t p[TERMS][2];     // probabilities of tile t - 1
+    bf16x8_t p[PT][2];        // probabilities of tile t - 1
 #pragma unroll
-    for (int i = 0; i < TERMS; ++i)
+    for (int i = 0; i < PT; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) p[i][h] = bf16x8_t{};
-    constexpr int N1 = TERMS * KK, N2 = TERMS * 2 * NB;   // MFMAs of the scores, of the values
+    constexpr int N1 = TERMS * KK, N2 = PT * 2 * NB;      // MFMAs of the scores, of the values
     constexpr int EXPS = 8, EXPS1 = EXPS * (N1 + N1 / 8) / (N1 + N2);   // pieces of the softmax (two scores each): behind the scores
 
     bf16x8_t kf[KK];   // of tile t + 1
@@ -728,7 +730,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
             continue;
         }
         f32x16_t n;
-        u32x4 pn[TERMS][2];
+        u32x4 pn[PT][2];
         bf16x8_t vf[2 * NB];
         const float ref = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
@@ -738,10 +740,11 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
             const float w0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale, -ref)), w1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale, -ref));
             sum += w0;
             sum += w1;
-            uint32_t w[TERMS];
-            cut_terms2<TERMS>(w0, w1, w);
+            uint32_t w[PT];
+            if constexpr (PT == TERMS) cut_terms2<PT>(w0, w1, w);
+            else round_terms2<PT>(w0, w1, w);
 #pragma unroll
-            for (int j = 0; j < TERMS; ++j) pn[j][e / 4][e % 4] = w[j];
+            for (int j = 0; j < PT; ++j) pn[j][e / 4][e % 4] = w[j];
             asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)
         };
         __builtin_amdgcn_sched_barrier(0);
@@ -769,7 +772,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < N2; ++c) {
-            const int f = c / TERMS, i = c % TERMS;   // fragment (h, b) = (f / NB, f % NB)
+            const int f = c % (2 * NB), i = PT - 1 - c / (2 * NB);   // small terms first; fragment (h, b) = (f / NB, f % NB)
             o[f % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], p[i][f / NB], o[f % NB], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -793,7 +796,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
         l += sum;
         s = n;
 #pragma unroll
-        for (int i = 0; i < TERMS; ++i)
+        for (int i = 0; i < PT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) p[i][h] = __builtin_bit_cast(bf16x8_t, pn[i][h]);
         raise(top, p);

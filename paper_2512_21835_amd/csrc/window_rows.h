@@ -88,6 +88,10 @@ __device__ __forceinline__ float4 quotient(float4 o, float l) {
     return make_float4(o.x * r, o.y * r, o.z * r, o.w * r);
 }
 
+// bf16 terms of a probability, by those of q: three with fp32 rows.  With bf16 rows two, which hold it to 2^-16 of its value,
+// well below a step of the output; one alone leaves 2^-8 in every product, and the output as far off again as its own rounding.
+constexpr int p_terms(int q_terms) { return q_terms == 1 ? 2 : q_terms; }
+
 // Term t of x as a sum of bf16 terms, each the nearest to what the ones before leave: three terms hold all 24 bits.
 template <int TERMS>
 __device__ __forceinline__ void split_terms(float x, __bf16 t[TERMS]) {
@@ -113,6 +117,19 @@ __device__ __forceinline__ void cut_terms2(float a, float b, uint32_t t[TERMS]) 
             a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
             b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
         }
+    }
+}
+
+// The same by rounding: what two terms leave is 2^-16 of the number at most, and on either side of it.
+template <int TERMS>
+__device__ __forceinline__ void round_terms2(float a, float b, uint32_t t[TERMS]) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i) {
+        t[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+        if (i == TERMS - 1) break;
+        a -= __uint_as_float(t[i] << 16);
+        b -= __uint_as_float(t[i] & 0xFFFF0000u);
     }
 }
 
