@@ -1,6 +1,8 @@
 // Window attention of prompts over an fp32 cache.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "lds_dma.h"
 #include "window_rows.h"
 
@@ -9,31 +11,32 @@ namespace {
 
 // A workgroup: 128 columns = G heads x BQ = 128 / G consecutive rows of one sequence, one KV head; wavefront w the
 // columns 32 w .. 32 w + 31 (column r: head r / BQ, row r % BQ).  K and V come in tiles of 32 keys (two pages): fp32 into
-// registers a tile ahead, from there as PL bf16 planes, whose sum they are, into one of two LDS stages.  S^T = K Q^T and
+// registers a tile ahead, from there as bf16 planes, K as three, whose sum it is, into one of two LDS stages.  S^T = K Q^T and
 // O^T += V^T P^T with 32x32x16 MFMAs, lane l holding keys 8 (i / 4) + 4 (l / 32) + i % 4 of the tile for column l % 32, the
 // k order of the operand P^T.
 //
 // fp32 rows: three terms of q and p against three planes hold all 24 bits of each; of the nine products the six largest are
-// taken; the others are at most 2^-23 of the whole.  bf16 rows: q is its one term, p one rounding to bf16
-// (2^-9 of a probability, as everywhere with bf16 rows) and two planes, 2^-16, are well below that.
+// taken; the others are at most 2^-23 of the whole.  bf16 rows: q is its one term, so that scores are as exact; p and V are two
+// terms each, rounded, which hold both to 2^-16 of their values, as p of bf16 rows everywhere.
 //
 // In turn t: K of tile t + 1 by Q, then V of tile t - 1 by P, and between their MFMAs the softmax of tile t, the terms of
 // K of tile t + 2 and of V of tile t.  2 x 600 fp32 rows of 40 heads behind 300 tokens, window 256: 106 us, 0.6 PFLOP/s
 // issued over whole tiles.  A turn takes 3.2 us, 1.6 of them MFMAs, alone on its SIMD (three terms of q, 96 registers, leave
 // no room for a second wavefront), and 400 workgroups are two rounds of 256.  Without the overlap 111 us; 16 columns at a
-// time with fp32 MFMAs (window_split) 262 us.
-template <int D, int PL>
+// time with fp32 MFMAs (window_split) 262 us.  bf16 rows: 82 us (69 with K and V as two cut planes and p as one term).
+template <int D, int V_PL>
 struct PlaneLds {
-    static constexpr int ROW = 2 * D, HALF = kTileKeys * ROW, PLANE = 2 * HALF, BYTES = PL * PLANE;   // K and V of a plane
+    static constexpr int K_PL = 3, ROW = 2 * D, PLANE = kTileKeys * ROW, V = K_PL * PLANE, BYTES = V + V_PL * PLANE;   // K's planes, V's
     static constexpr int CHUNKS = D / 64;   // chunks of 8 elements per thread: key tid / 8, chunks tid % 8 + 8 i
     __device__ static int kx(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
     __device__ static int vx(int key) { return D == 128 ? (key & 3) << 2 : (key & 2) << 1; }
 };
 
-template <int D, int TERMS, int PL>
+template <int D, int TERMS>
 __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log_g) {
-    using L = PlaneLds<D, PL>;
-    constexpr int KK = D / 16, NB = D / 32, TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32;
+    constexpr int PT = p_terms(TERMS), V_PL = PT, KK = D / 16, NB = D / 32;
+    using L = PlaneLds<D, V_PL>;
+    constexpr int K_PL = L::K_PL, TYPE = TERMS == 1 ? STAGE_BF16 : STAGE_F32;
     __shared__ __align__(1024) char lds[2 * L::BYTES];
     __shared__ int flags[4];
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -77,25 +80,29 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         block_k[1] = __builtin_amdgcn_readlane(ids, 2 * (t % 32) + (wave >> 1));
         fetch(raw_k, block_k[1], 0);
     };
-    // A K or V that is not finite becomes 0: the columns that see it, if any does, are taken again at the end.
+    // A K or V that is not finite (or too large to be rounded to bf16) becomes 0: the columns that see it, if any does, are taken again at the end.
     bool odd = false, bad_k = false, bad_v = false;
     const int my_key = 8 * wave + lane / 8;
     const uint32_t k_to = base + my_key * L::ROW + 16 * (lane % 8 ^ L::kx(my_key));
-    const uint32_t v_to = base + L::HALF + my_key * L::ROW + 16 * (lane % 8 ^ L::vx(my_key));
-    u32x4 planes[PL];
+    const uint32_t v_to = base + L::V + my_key * L::ROW + 16 * (lane % 8 ^ L::vx(my_key));
+    u32x4 planes[K_PL];
+    using KPlanes = std::integral_constant<int, K_PL>;
+    using VPlanes = std::integral_constant<int, V_PL>;
     constexpr int PIECES = 4 * L::CHUNKS;   // two elements each
-    auto convert = [&](const f32x4_t(&raw)[L::CHUNKS][2], uint32_t to, int piece, bool &any_bad) {
+    auto convert = [&](auto n, const f32x4_t(&raw)[L::CHUNKS][2], uint32_t to, int piece, bool &any_bad) {
+        constexpr int PL = decltype(n)::value;
         const int i = piece / 4, e0 = piece % 4 * 2;
         float x[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             x[e] = raw[i][e0 / 4][e0 % 4 + e];
-            const bool bad = !(fabsf(x[e]) < INFINITY);
+            const bool bad = !(fabsf(x[e]) <= kMaxBf16);
             any_bad |= bad;
             x[e] = bad ? 0.f : x[e];
         }
         uint32_t w[PL];
-        cut_terms2<PL>(x[0], x[1], w);
+        if constexpr (PL == K_PL) cut_terms2<PL>(x[0], x[1], w);
+        else round_terms2<PL>(x[0], x[1], w);
 #pragma unroll
         for (int p = 0; p < PL; ++p) planes[p][e0 / 2] = w[p];
         if (e0 == 6) {
@@ -142,7 +149,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
     const float scale = fabsf(a.scale) * kLog2e;   // scores in base 2
     const uint32_t k_at = base + col * L::ROW + 16 * (half ^ L::kx(col));   // chunk 2 kk + half of key col, permuted
     const int vk = 4 * half + (lane & 15) / 4;
-    const uint32_t v_at = base + L::HALF + vk * L::ROW + 8 * (lane & 1) + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ L::vx(vk));
+    const uint32_t v_at = base + L::V + vk * L::ROW + 8 * (lane & 1) + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ L::vx(vk));
     auto value_frag = [&](uint32_t v, int h, int b) {
         const uint32_t from = (v ^ (64 * b)) + 16 * h * L::ROW;
         const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds8)from);
@@ -158,9 +165,9 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             pages = (known(seq.table[rb.page_at(t, 0)]) ? 0xFFFFu : 0u) | (known(seq.table[rb.page_at(t, 1)]) ? 0xFFFF0000u : 0u);
         hide_scores(x, pages >> (4 * half) & seen_bits(a, pos, rb.tile_at(t) * kTileKeys + 4 * half));
     };
-    bf16x8_t p[TERMS][2];   // probabilities of tile t - 1
+    bf16x8_t p[PT][2];   // probabilities of tile t - 1
 #pragma unroll
-    for (int i = 0; i < TERMS; ++i)
+    for (int i = 0; i < PT; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) p[i][h] = bf16x8_t{};
     // The maximum: a whole number that stays until a score is 2^kSlack beyond it, so that rescaling is exact, and rare.
@@ -176,36 +183,36 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
 #pragma unroll
-        for (int i = 0; i < TERMS; ++i)
+        for (int i = 0; i < PT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) p[i][h][j] = (__bf16)((float)p[i][h][j] * alpha);
     };
     // Groups of MFMAs of one fragment (small terms first), the fragments read AHEAD groups before theirs.
-    constexpr int N = PL * KK, M = 2 * PL * NB, AHEAD = PL;
+    constexpr int N = K_PL * KK, M = 2 * V_PL * NB, AHEAD = K_PL;
     auto key_frag = [&](uint32_t stage, int c) {
-        return __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + stage + (PL - 1 - c % PL) * L::PLANE) ^ (32 * (c / PL))));
+        return __builtin_bit_cast(bf16x8_t, *(lds16)((k_at + stage + (K_PL - 1 - c % K_PL) * L::PLANE) ^ (32 * (c / K_PL))));
     };
-    auto value_of = [&](uint32_t stage, int c) { return value_frag(v_at + stage + (PL - 1 - c / NB % PL) * L::PLANE, c / NB / PL, c % NB); };
+    auto value_of = [&](uint32_t stage, int c) { return value_frag(v_at + stage + (V_PL - 1 - c / NB % V_PL) * L::PLANE, c / NB / V_PL, c % NB); };
     auto key_products = [&](f32x16_t &x, const bf16x8_t &k, int c) {
 #pragma unroll
         for (int i = TERMS - 1; i >= 0; --i)
-            if (i + PL - 1 - c % PL < PL) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][c / PL], x, 0, 0, 0);
+            if (i + K_PL - 1 - c % K_PL < K_PL) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][c / K_PL], x, 0, 0, 0);
     };
 
     // K of tiles 0 and 1 to their stages; zeros where turn 0 looks for the V of a tile before
 #pragma unroll
-    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to, e, bad_k);
+    for (int e = 0; e < PIECES; ++e) convert(KPlanes{}, raw_k, k_to, e, bad_k);
     noted(bad_k, 0);
     fetch_k(1);
 #pragma unroll
-    for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + L::BYTES, e, bad_k);
+    for (int e = 0; e < PIECES; ++e) convert(KPlanes{}, raw_k, k_to + L::BYTES, e, bad_k);
     noted(bad_k, 1);
 #pragma unroll
     for (int i = 0; i < L::CHUNKS; ++i)
 #pragma unroll
-        for (int c = 0; c < PL; ++c) *(lds16)((v_to ^ (128 * i)) + L::BYTES + c * L::PLANE) = u32x4{0, 0, 0, 0};
+        for (int c = 0; c < V_PL; ++c) *(lds16)((v_to ^ (128 * i)) + L::BYTES + c * L::PLANE) = u32x4{0, 0, 0, 0};
     fetch_k(2);
     wait_lgkm<0>();
     lds_barrier();
@@ -230,17 +237,17 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         const uint32_t even = (t & 1) * L::BYTES, odd_stage = L::BYTES - even;   // stages of tiles t and t + 2; of t + 1 and t - 1
         if (!mine.has(t)) {   // (p is 0 then, and s -inf)
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) convert(raw_k, k_to + even, e, bad_k);
+            for (int e = 0; e < PIECES; ++e) convert(KPlanes{}, raw_k, k_to + even, e, bad_k);
             noted(bad_k, t + 2);
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) convert(raw_v, v_to + even, e, bad_v);
+            for (int e = 0; e < PIECES; ++e) convert(VPlanes{}, raw_v, v_to + even, e, bad_v);
             noted(bad_v, t);
             if (t + 1 < n_tiles) fetch(raw_v, block_k[0], hkv * head);
             fetch_k(t + 3);
             continue;
         }
         f32x16_t n;   // scores of tile t + 1
-        u32x4 pn[TERMS][2];
+        u32x4 pn[PT][2];
         bf16x8_t f[AHEAD];
         const float ref = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
@@ -250,10 +257,11 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             const float w0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale, -ref)), w1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale, -ref));
             sum += w0;
             sum += w1;
-            uint32_t w[TERMS];
-            cut_terms2<TERMS>(w0, w1, w);
+            uint32_t w[PT];
+            if constexpr (PT == TERMS) cut_terms2<PT>(w0, w1, w);
+            else round_terms2<PT>(w0, w1, w);
 #pragma unroll
-            for (int j = 0; j < TERMS; ++j) pn[j][e / 4][e % 4] = w[j];
+            for (int j = 0; j < PT; ++j) pn[j][e / 4][e % 4] = w[j];
             asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)
         };
 #pragma unroll
@@ -266,7 +274,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             else f[c % AHEAD] = value_of(odd_stage, c + AHEAD - N);
 #pragma unroll
             for (int e = 0; e < PIECES; ++e)
-                if (e * N / PIECES == c) convert(raw_k, k_to + even, e, bad_k);
+                if (e * N / PIECES == c) convert(KPlanes{}, raw_k, k_to + even, e, bad_k);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e * N / 4 + 1 == c) softmax_piece(e);
@@ -280,15 +288,15 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         static_assert(N % AHEAD == 0, "the values' first fragments follow the keys' last");
 #pragma unroll
         for (int c = 0; c < M; ++c) {
-            const int b = c % NB, h = c / NB / PL, pl = PL - 1 - c / NB % PL;
+            const int b = c % NB, h = c / NB / V_PL, pl = V_PL - 1 - c / NB % V_PL;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = TERMS - 1; i >= 0; --i)
-                if (i + pl < PL) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[c % AHEAD], p[i][h], o[b], 0, 0, 0);
+            for (int i = PT - 1; i >= 0; --i)
+                if (PT < 3 || i + pl < 3) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[c % AHEAD], p[i][h], o[b], 0, 0, 0);
             if (c + AHEAD < M) f[c % AHEAD] = value_of(odd_stage, c + AHEAD);
 #pragma unroll
             for (int e = 0; e < PIECES; ++e)
-                if (e * M / PIECES == c) convert(raw_v, v_to + even, e, bad_v);
+                if (e * M / PIECES == c) convert(VPlanes{}, raw_v, v_to + even, e, bad_v);
 #pragma unroll
             for (int e = 4; e < 8; ++e)
                 if ((e - 4) * M / 4 + 1 == c) softmax_piece(e);
@@ -302,7 +310,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
         l += sum;
         s = n;
 #pragma unroll
-        for (int i = 0; i < TERMS; ++i)
+        for (int i = 0; i < PT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) p[i][h] = __builtin_bit_cast(bf16x8_t, pn[i][h]);
         raise(top);
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             load4(k, 16 * kk + 8 * half + 4, STAGE_F32, y + 4);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                bad |= !(fabsf(y[j]) < INFINITY);
+                bad |= !(fabsf(y[j]) <= kMaxBf16);
                 w = fmaf(x[j], y[j], w);
             }
             asm volatile("" ::: "memory");   // (registers)
@@ -371,7 +379,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
                 load4(v, 32 * c + 8 * j + 4 * half, STAGE_F32, x);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    bad |= !(fabsf(x[e]) < INFINITY);
+                    bad |= !(fabsf(x[e]) <= kMaxBf16);
                     o[c][4 * j + e] = o[c][4 * j + e] * alpha + (seen ? w * x[e] : 0.f);
                 }
                 __builtin_amdgcn_sched_barrier(0);   // (registers)
@@ -381,7 +389,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
     if (__shfl_xor((int)again, 32) | (int)again) store();
 }
 
-template <int D, int TERMS, int PL>
+template <int D, int TERMS>
 hipError_t launch(const WindowArgs &a, hipStream_t st) {
     int log_g = 0;
     while (a.n_kv_heads << log_g < a.n_q_heads) ++log_g;
@@ -389,7 +397,7 @@ hipError_t launch(const WindowArgs &a, hipStream_t st) {
     const int bq = 128 >> log_g, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
     const long blocks = ((long)a.rows.rows / bq + seqs) * a.n_kv_heads;
     if (blocks > kMaxBlocks) return hipErrorInvalidValue;
-    STG_LAUNCH((window_tiles_f32<D, TERMS, PL>), dim3((unsigned)blocks), dim3(256), 0, st, a, log_g);
+    STG_LAUNCH((window_tiles_f32<D, TERMS>), dim3((unsigned)blocks), dim3(256), 0, st, a, log_g);
     return hipGetLastError();
 }
 
@@ -397,8 +405,8 @@ hipError_t launch(const WindowArgs &a, hipStream_t st) {
 
 hipError_t launch_window_f32(const WindowArgs &a, hipStream_t st) {
     const bool exact = a.type == STAGE_F32;
-    if (a.head_dim == 64) return exact ? launch<64, 3, 3>(a, st) : launch<64, 1, 2>(a, st);
-    if (a.head_dim == 128) return exact ? launch<128, 3, 3>(a, st) : launch<128, 1, 2>(a, st);
+    if (a.head_dim == 64) return exact ? launch<64, 3>(a, st) : launch<64, 1>(a, st);
+    if (a.head_dim == 128) return exact ? launch<128, 3>(a, st) : launch<128, 1>(a, st);
     return hipErrorInvalidValue;
 }
 

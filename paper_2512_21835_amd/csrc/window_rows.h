@@ -27,6 +27,7 @@ constexpr int kPage = kBlockTokens;
 constexpr long kMaxBlocks = (1L << 24) - 1;   // workgroups of 256 in a grid: their threads are counted in 32 bits
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;
+constexpr float kMaxBf16 = 0x1.FEp127f;
 
 // The same in every lane, and known to be.
 __device__ __forceinline__ OpRows::Seq uniform(OpRows::Seq s) {

@@ -22,3 +22,39 @@ def test_probabilities_of_bf16_rows(rows, held, hq, hkv, d, window, sinks):
     got = _run_window(c, window, sinks)
     want, off32, off16 = O.window(b, q, out, b.pool, hq, window, sinks)
     O.assert_within(got, want, O.rounded(want, off32 + off16 * 2.0 ** -8, torch.bfloat16))
+
+
+# heads that make these whole tiles of rows, and those that do not
+F32_CACHE = [([1, 1, 1], [5, 300, 900], 8, 2), ([37, 1, 70], [90, 0, 200], 72, 9), ([37, 70, 60, 50], [90, 200, 0, 7], 50, 50)]
+
+
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (64, 3)])
+def test_probabilities_and_values_of_bf16_rows_over_an_fp32_cache(rows, held, hq, hkv, d, window, sinks):
+    """As above, and V as two terms too: 2^-16 twice."""
+    b, q, out = c = _window_case(rows, held, hq, hkv, d, "bf16", "fp32")
+    got = _run_window(c, window, sinks)
+    want, off32, off16 = O.window(b, q, out, b.pool, hq, window, sinks)
+    O.assert_within(got, want, O.rounded(want, off32 + 2 * off16 * 2.0 ** -8, torch.bfloat16))
+
+
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_of_bf16_rows_over_an_fp32_cache(rows, held, hq, hkv, d):
+    """Scores of 200 from one product each, q of one element: half the keys' K are 4 and half the next number below, with V of
+    the other sign, so that the output is what the scores are off.  A score's error does not grow with d here: three
+    exact products and their sums, the scale in base 2 and the product by it: 8 of the 8 + d steps that the oracle takes."""
+    b, q, out = c = _window_case(rows, held, hq, hkv, d, "bf16", "fp32")
+    q.zero_()
+    q[..., 5] = 50
+    places = torch.arange(16) % 2 == 0
+    b.pool[:, 0] = torch.where(places[:, None], 4.0, torch.nextafter(torch.tensor(4.0), torch.tensor(0.0)))
+    b.pool[:, 1] = torch.where(places[:, None], 1.0, -1.0) * (1 + torch.rand(hkv, 1, d, generator=b.gen))
+    got = _run_window(c, 0, 0, scale=1.0)
+    want, off32, off16 = O.window(b, q, out, b.pool, hq, 0, 0, 1.0)
+    keys = torch.tensor([n - r + t + 1 for n, r in zip(b.lengths, b.rows) for t in range(r)]).view(-1, 1, 1).double()
+    term = off16 / O.U16
+    size = (off32 / (term * O.U32) - 2 * keys - 32) / (2 * (d + 8))
+    off = term * O.U32 * (2 * 16 * size + 2 * keys + 32) + 2 * off16 * 2.0 ** -8
+    O.assert_within(got, want, O.rounded(want, off, torch.bfloat16))
