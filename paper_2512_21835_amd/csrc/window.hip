@@ -499,7 +499,7 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
 // probabilities' second term; with one term, the output off by its own rounding once more, 286 us).  What is not loop is
 // beginning (block search, page ids, first tiles: 3 to 4 us a workgroup), end, and the halves of tiles outside the window.
 // 256 columns a workgroup (each wavefront 64) are slower: one wavefront per SIMD hides less than two.  fp32 rows issue three
-// times the products: 12 prompts of up to 500 rows, window 512, 122 us.
+// times the products: 12 prompts of up to 500 rows, window 512, 123 us.
 template <int D>
 struct TileLds {
     static constexpr int KEYS = 32, ROW = 2 * D, HALF = KEYS * ROW, BYTES = 2 * HALF, CH = ROW / 16;
@@ -741,8 +741,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
             sum += w0;
             sum += w1;
             uint32_t w[PT];
-            if constexpr (PT == TERMS) cut_terms2<PT>(w0, w1, w);
-            else round_terms2<PT>(w0, w1, w);
+            split_terms2<PT>(w0, w1, w);
 #pragma unroll
             for (int j = 0; j < PT; ++j) pn[j][e / 4][e % 4] = w[j];
             asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)

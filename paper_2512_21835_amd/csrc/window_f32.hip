@@ -16,14 +16,15 @@ namespace {
 // k order of the operand P^T.
 //
 // fp32 rows: three terms of q and p against three planes hold all 24 bits of each; of the nine products the six largest are
-// taken; the others are at most 2^-23 of the whole.  bf16 rows: q is its one term, so that scores are as exact; p and V are two
+// taken; the others are at most 2^-24 of the whole, of either sign (terms cut from the bits, always toward zero, would leave
+// 2^-21).  bf16 rows: q is its one term, so that scores are as exact; p and V are two
 // terms each, rounded, which hold both to 2^-16 of their values, as p of bf16 rows everywhere.
 //
 // In turn t: K of tile t + 1 by Q, then V of tile t - 1 by P, and between their MFMAs the softmax of tile t, the terms of
-// K of tile t + 2 and of V of tile t.  2 x 600 fp32 rows of 40 heads behind 300 tokens, window 256: 106 us, 0.6 PFLOP/s
+// K of tile t + 2 and of V of tile t.  2 x 600 fp32 rows of 40 heads behind 300 tokens, window 256: 108 us, 0.6 PFLOP/s
 // issued over whole tiles.  A turn takes 3.2 us, 1.6 of them MFMAs, alone on its SIMD (three terms of q, 96 registers, leave
 // no room for a second wavefront), and 400 workgroups are two rounds of 256.  Without the overlap 111 us; 16 columns at a
-// time with fp32 MFMAs (window_split) 262 us.  bf16 rows: 82 us (69 with K and V as two cut planes and p as one term).
+// time with fp32 MFMAs (window_split) 262 us.  bf16 rows: 85 us (69 with K and V as two cut planes and p as one term).
 template <int D, int V_PL>
 struct PlaneLds {
     static constexpr int K_PL = 3, ROW = 2 * D, PLANE = kTileKeys * ROW, V = K_PL * PLANE, BYTES = V + V_PL * PLANE;   // K's planes, V's
@@ -101,8 +102,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             x[e] = bad ? 0.f : x[e];
         }
         uint32_t w[PL];
-        if constexpr (PL == K_PL) cut_terms2<PL>(x[0], x[1], w);
-        else round_terms2<PL>(x[0], x[1], w);
+        split_terms2<PL>(x[0], x[1], w);
 #pragma unroll
         for (int p = 0; p < PL; ++p) planes[p][e0 / 2] = w[p];
         if (e0 == 6) {
@@ -258,8 +258,7 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             sum += w0;
             sum += w1;
             uint32_t w[PT];
-            if constexpr (PT == TERMS) cut_terms2<PT>(w0, w1, w);
-            else round_terms2<PT>(w0, w1, w);
+            split_terms2<PT>(w0, w1, w);
 #pragma unroll
             for (int j = 0; j < PT; ++j) pn[j][e / 4][e % 4] = w[j];
             asm volatile("" : "+v"(sum));   // (here, and not where the sums are needed)

@@ -93,7 +93,8 @@ __device__ __forceinline__ float4 quotient(float4 o, float l) {
 // well below a step of the output; one alone leaves 2^-8 in every product, and the output as far off again as its own rounding.
 constexpr int p_terms(int q_terms) { return q_terms == 1 ? 2 : q_terms; }
 
-// Term t of x as a sum of bf16 terms, each the nearest to what the ones before leave: three terms hold all 24 bits.
+// x as a sum of bf16 terms, each the nearest to what the ones before leave: term 1 is at most 2^-8 of x, term 2 2^-17, and
+// three hold all 24 bits.
 template <int TERMS>
 __device__ __forceinline__ void split_terms(float x, __bf16 t[TERMS]) {
 #pragma unroll
@@ -103,27 +104,9 @@ __device__ __forceinline__ void split_terms(float x, __bf16 t[TERMS]) {
     }
 }
 
-// Two numbers (a in the low halves) at once.  One term is the nearest bf16; several are cut from the bits, each the leading
-// 8 of what the ones before leave, so three hold all 24 as well, in fewer instructions than by rounding.
+// Two numbers (a in the low halves) at once.
 template <int TERMS>
-__device__ __forceinline__ void cut_terms2(float a, float b, uint32_t t[TERMS]) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    if constexpr (TERMS == 1) {
-        t[0] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    } else {
-#pragma unroll
-        for (int i = 0; i < TERMS; ++i) {
-            t[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-            if (i == TERMS - 1) break;
-            a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
-            b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-        }
-    }
-}
-
-// The same by rounding: what two terms leave is 2^-16 of the number at most, and on either side of it.
-template <int TERMS>
-__device__ __forceinline__ void round_terms2(float a, float b, uint32_t t[TERMS]) {
+__device__ __forceinline__ void split_terms2(float a, float b, uint32_t t[TERMS]) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < TERMS; ++i) {

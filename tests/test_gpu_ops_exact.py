@@ -58,3 +58,17 @@ def test_scores_of_bf16_rows_over_an_fp32_cache(rows, held, hq, hkv, d):
     size = (off32 / (term * O.U32) - 2 * keys - 32) / (2 * (d + 8))
     off = term * O.U32 * (2 * 16 * size + 2 * keys + 32) + 2 * off16 * 2.0 ** -8
     O.assert_within(got, want, O.rounded(want, off, torch.bfloat16))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+def test_rows_that_see_one_value_give_it(rows, held, hq, hkv, d, cache):
+    """A window of one token: p V / p, with V of as many ones as its terms can have.  Off by 2^-24 of V for the products of
+    small terms that are left out, two steps of the sum, the reciprocal and the product by it: 5 half steps of fp32."""
+    b, q, out = c = _window_case(rows, held, hq, hkv, d, "fp32", cache)
+    sign = torch.randint(0, 2, b.pool[:, 1].shape, generator=b.gen) * 2.0 - 1
+    b.pool[:, 1] = sign * (1 + 2.0 ** -7 - 2.0 ** -23) * 2.0 ** torch.randint(-3, 4, sign.shape, generator=b.gen)
+    got = _run_window(c, 1, 0)
+    want = O.window(b, q, out, b.pool, hq, 1, 0)[0]
+    O.assert_within(got, want, 5 * O.U32 * want.abs())
