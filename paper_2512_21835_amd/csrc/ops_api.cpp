@@ -196,6 +196,7 @@ int stage_window_attention(const stage_window_args *p, void *workspace, int64_t 
     if (!window_sizes(a) || !pointers_ok(a.batch, a.cache)) return STAGE_EINVAL;
     const int64_t width = (int64_t)a.n_q_heads * a.cache.head_dim;
     if (!rows_ok(a.q, a.q_ld, width, a.type) || !rows_ok(a.out, a.out_ld, width, a.type)) return STAGE_EINVAL;
+    if (a.out == a.q && a.out_ld != a.q_ld) return STAGE_EINVAL;
     if (!device_ok(a.device)) return STAGE_EINVAL;
     DeviceGuard dg(a.device);
     const WindowArgs w = window_args(a, workspace);

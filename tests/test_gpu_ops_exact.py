@@ -3,7 +3,7 @@
 import pytest
 import torch
 
-import paper_2512_21835_amd as P  # noqa: F401
+import paper_2512_21835_amd as P
 from tests import ops_oracle as O
 from tests.test_gpu_ops import _run_window, _window_case
 
@@ -72,3 +72,32 @@ def test_rows_that_see_one_value_give_it(rows, held, hq, hkv, d, cache):
     got = _run_window(c, 1, 0)
     want = O.window(b, q, out, b.pool, hq, 1, 0)[0]
     O.assert_within(got, want, 5 * O.U32 * want.abs())
+
+
+def _same(a, b):
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+
+
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+def test_window_in_place(rows, held, hq, hkv, cache, act):
+    """out is q: the same bits, where a K and a V that some rows see are not finite as well."""
+    b, q, out = c = _window_case(rows, held, hq, hkv, 64, act, cache)
+    for poisoned in (False, True):
+        if poisoned:
+            for what, i, back in ((0, 0, 1), (1, len(rows) - 1, 3)):
+                p = b.lengths[i] - back
+                b.pool[int(b.table[i, p // 16]), what, 0, p % 16, 9] = float("inf")
+        want = _run_window(c, 40, 2)
+        x = q.cuda()
+        P.stage_window_attention(x, x, b.pool.cuda(), b.stage_batch(P), window=40, sinks=2)
+        assert _same(x, want), poisoned
+
+
+def test_window_in_place_with_another_stride_is_refused():
+    b, q, out = _window_case([2], [3], 4, 2, 64, "fp32", "bf16")
+    wide = torch.zeros(4, 4, 64, device="cuda")
+    with pytest.raises(P.StageError) as e:
+        P.stage_window_attention(wide[:2], wide[::2], b.pool.cuda(), b.stage_batch(P))
+    assert e.value.code == P.STAGE_EINVAL
