@@ -103,8 +103,9 @@ int stage_norm_rope_append(const stage_append_args *a, void *stream);
    n_kv_heads).  Products, softmax statistics and sums are in fp32 or more exact: with fp32 activations the
    operands of the matrix instructions are exact sums of bf16 terms (or fp32, with an fp32 cache); with bf16
    activations the probabilities, and the values of an fp32 cache, may be held to 2^-16 of their sizes.  Nothing of
-   a place that a row does not see reaches its result, infinities and NaN among it.  Tokens in blocks whose id is not one
-   of the pool's are not seen; a row that sees none (its position is negative, say) becomes 0.  out may be q itself, with
+   a place that a row does not see reaches its result, infinities and NaN among it; those that it sees give what they give
+   in the formula.  Tokens in blocks whose id is not one of the pool's are not seen; a row that sees none (its position is
+   negative, say) becomes 0.  out may be q itself, with
    the same stride; else they share no element. */
 typedef struct {
     int32_t device;

@@ -106,6 +106,62 @@ struct Columns {
         }
     }
 
+    // The columns whose state is not finite once more, key by key in fp32: of an infinity or a number too large for bf16 the
+    // terms are none (inf - inf).  pool: of the KV head.  (An fp32 cache's products have no terms.)
+    __device__ __forceinline__ void by_keys(const WindowArgs &a, const uint16_t *pool, const int *table, const Span &sp, int beg, int end,
+                                            size_t q_at, bool valid) {
+        uint32_t most = size_bits(l);
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = max(most, size_bits(o[b][i]));
+        const int lane = __lane_id(), lq = lane >> 4;
+        const uint64_t lanes = __builtin_amdgcn_ballot_w64(valid & (most >= 0x7F800000u));
+        if (lanes == 0) return;
+        const size_t head = (size_t)kPage * D;
+        f32x4_t o2[D / 16];
+        float m2 = -INFINITY, l2 = 0.f;
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b) o2[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int u = beg * kPage; u < end * kPage; ++u) {
+            const int page = sp.page(u / kPage), key = page * kPage + u % kPage, block = ((const_ints)(uintptr_t)table)[page];
+            if ((unsigned)block >= (unsigned)a.rows.n_blocks) continue;
+            const size_t k = (size_t)block * 2 * a.n_kv_heads * head + u % kPage * D + 4 * lq, v = k + a.n_kv_heads * head;
+            float w = 0.f;
+#pragma unroll
+            for (int b = 0; b < D / 16; ++b) {
+                float x[4], y[4];
+                load4(a.q, q_at + 16 * b + 4 * lq, a.type, x);
+                load4(pool, k + 16 * b, STAGE_BF16, y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w = fmaf(x[i], y[i], w);
+            }
+            w += lane_xor(w, 16);
+            w += lane_xor(w, 32);
+            w *= a.scale * kLog2e;
+            const bool seen = sees(a, pos, key);
+            const float to = seen & (w > m2) ? w : m2, ref = to == -INFINITY ? 0.f : to;
+            const float alpha = __builtin_amdgcn_exp2f(m2 - ref);
+            w = seen ? __builtin_amdgcn_exp2f(w - ref) : 0.f;
+            m2 = to;
+            l2 = l2 * alpha + (lq == 0 ? w : 0.f);
+#pragma unroll
+            for (int b = 0; b < D / 16; ++b) {
+                float x[4];
+                load4(pool, v + 16 * b, STAGE_BF16, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o2[b][i] = o2[b][i] * alpha + (seen ? w * x[i] : 0.f);
+            }
+        }
+        if (lanes >> (lane & 15) & 0x0001000100010001ull) {
+            m = m2;
+            l = l2;
+#pragma unroll
+            for (int b = 0; b < D / 16; ++b) o[b] = o2[b];
+        }
+    }
+
     // lds: the page's image; k0: its first key; masked: some column does not see all of it; rows: of the block
     // (positions first .. first + rows - 1)
     __device__ __forceinline__ void add(const WindowArgs &a, uint32_t lds, int k0, bool masked, int first, int rows) {
@@ -354,6 +410,9 @@ __global__ __launch_bounds__(256) void window_split(WindowArgs a, SplitPlan pl) 
         const int k0 = sp.page(u) * kPage;
         cols.add(a, ring + u % S * L::BYTES, k0, !all_see(a, first, last, k0, kPage), first, rows);
     }
+
+    if constexpr (!F32)
+        cols.by_keys(a, reinterpret_cast<const uint16_t *>(pool), seq.table, sp, beg, end, row * a.q_ld + (size_t)h * D, t < rows);
 
     // the wavefronts' states meet in LDS
     float l = cols.l;
@@ -615,8 +674,8 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
     Turns mine = widened(rb.touched(a, w_first, max(w_first, w_last)));   // what the wavefront takes part in
     if (w_rows <= 0) mine = Turns{0, 0, 0};
     // This wavefront's share of tile t has landed; with the barrier behind it, everybody's.  In a tile that not every
-    // row sees, a V that is not finite must not meet the matrix instructions (0 x inf): it becomes 0 here, and is
-    // added at the end for the columns that see it.
+    // row sees, a V that is not finite must not meet the matrix instructions (0 x inf): it becomes 0 here, and the
+    // columns that see it are taken again at the end.
     auto landed = [&](int t, uint32_t at, int behind) {   // behind: tiles under way behind it
         if (S > 5 && behind >= 2) wait_vm<(S > 5 ? 2 : 1) * 2 * L::COPIES>();
         else if (S > 4 && behind >= 1) wait_vm<2 * L::COPIES>();
@@ -800,69 +859,42 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
             for (int h = 0; h < 2; ++h) p[i][h] = __builtin_bit_cast(bf16x8_t, pn[i][h]);
         raise(top, p);
     }
-    // whether any wavefront cleared a V
-    __syncthreads();
     int *const flags = reinterpret_cast<int *>(lds);
-    if (lane == 0) flags[wave] = 0;
-    if (odd) flags[wave] = 1;
-    __syncthreads();
-    if (flags[0] | flags[1] | flags[2] | flags[3]) {   // the cleared elements, key by key
-        const char *const gk = pool + 16 * half, *const gv = pool + hkv * head + 8 * half;
-#pragma unroll 1
-        for (int key = 0; key < n_tiles * KT; ++key) {
-            const int t = key / KT, k0 = rb.tile_at(t) * KT, at = k0 + key % KT, page = at / kPage;
-            if (page > last_page) continue;
-            const int b = ((const_ints)(uintptr_t)seq.table)[page];
-            if (!known(b) || (clear.has(t) && !strange)) continue;
-            const size_t place = (size_t)b * block_bytes + at % kPage * L::ROW;
-            float w = 0.f;
+    auto store = [&] {
+        // Rows are stored 16 bytes a lane, neighbouring lanes side by side, by way of the ring (8 bytes a lane, each row's
+        // over 16 instructions: 30 us more of 320 at 4 x 2048 rows of 64 heads).
+        constexpr int E = TYPE == STAGE_F32 ? 4 : 2, OROW = D * E + 16, OCH = D * E / 16;
+        static_assert(64 + 4 * 32 * OROW <= S * L::BYTES, "the ring holds the output rows");
+        char *const out_lds = lds + 64 + wave * 32 * OROW;   // (behind the flags)
+        const int out_type = TYPE == STAGE_F32 && seq.first + t0 + t < a.pair_rows ? kPair : TYPE;
+        const float sum = l + lane_xor(l, 32);
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(gk + place + 32 * kk);
-                float v[8];
-                load4(a.q, q_at + 16 * kk, TYPE, v);
-                load4(a.q, q_at + 16 * kk + 4, TYPE, v + 4);
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w = fmaf(v[j], (float)k[j], w);
-                asm volatile("" ::: "memory");   // (registers)
-            }
-            w += lane_xor(w, 32);
-            w = __builtin_amdgcn_exp2f(fmaf(w, a.scale * kLog2e, m == -INFINITY ? 0.f : -m));
-            if (!sees(a, pos, at)) continue;
+            for (int j = 0; j < 4; ++j)
+                store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, out_type,
+                       quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
 #pragma unroll
-            for (int c = 0; c < NB; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float v[4];
-                    load4(gv + place, 32 * c + 8 * j, STAGE_BF16, v);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        o[c][4 * j + i] = fabsf(v[i]) < INFINITY ? o[c][4 * j + i] : fmaf(w, v[i], o[c][4 * j + i]);
-                    __builtin_amdgcn_sched_barrier(0);   // (registers)
-                }
+        for (int i = 0; i < 32 * OCH / 64; ++i) {
+            const int e = 64 * i + lane, r = c0 + e / OCH, t = r & (bq - 1);
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(out_lds + e / OCH * OROW + e % OCH * 16);
+            if (t < rows)
+                *reinterpret_cast<u32x4 *>(static_cast<char *>(a.out) + E * ((size_t)(seq.first + t0 + t) * a.out_ld +
+                                           (size_t)((g << pl.log_g) + (r >> log_bq)) * D) + e % OCH * 16) = v;
         }
-    }
-    // Rows are stored 16 bytes a lane, neighbouring lanes side by side, by way of the ring (8 bytes a lane, each row's
-    // over 16 instructions: 30 us more of 320 at 4 x 2048 rows of 64 heads).
-    constexpr int E = TYPE == STAGE_F32 ? 4 : 2, OROW = D * E + 16, OCH = D * E / 16;
-    static_assert(64 + 4 * 32 * OROW <= S * L::BYTES, "the ring holds the output rows");
-    char *const out_lds = lds + 64 + wave * 32 * OROW;   // (behind the flags)
-    const int out_type = TYPE == STAGE_F32 && seq.first + t0 + t < a.pair_rows ? kPair : TYPE;
-    const float sum = l + lane_xor(l, 32);
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            store4(out_lds + col * OROW, 32 * b + 8 * j + 4 * half, out_type,
-                   quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
-#pragma unroll
-    for (int i = 0; i < 32 * OCH / 64; ++i) {
-        const int e = 64 * i + lane, r = c0 + e / OCH, t = r & (bq - 1);
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(out_lds + e / OCH * OROW + e % OCH * 16);
-        if (t < rows)
-            *reinterpret_cast<u32x4 *>(static_cast<char *>(a.out) + E * ((size_t)(seq.first + t0 + t) * a.out_ld +
-                                       (size_t)((g << pl.log_g) + (r >> log_bq)) * D) + e % OCH * 16) = v;
-    }
+    };
+    // Columns that see a V that was cleared, or whose sums are not finite, are taken again; the others keep what they
+    // have.  (Rows are stored before, unless out is q, which is read again.)
+    const bool same = a.out == a.q;
+    __syncthreads();
+    if (!same) store();
+    const bool bad = t < rows && not_finite(l, o);
+    if (lane == 0) flags[wave] = 0;
+    if (odd | bad) flags[wave] = 1;
+    __syncthreads();
+    const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+    if (__builtin_expect(any, 0)) by_keys<D, TYPE, STAGE_BF16>(a, rb, g, q_at, pos, bad, o, l);
+    if (__builtin_expect(any | same, 0)) store();
 }
 
 template <int D, int TERMS>

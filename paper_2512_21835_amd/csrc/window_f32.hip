@@ -314,80 +314,29 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
             for (int h = 0; h < 2; ++h) p[i][h] = __builtin_bit_cast(bf16x8_t, pn[i][h]);
         raise(top);
     }
-    if (lane == 0) flags[wave] = 0;
-    if (odd) flags[wave] = 1;
-    __syncthreads();
-    if (flags[0] | flags[1] | flags[2] | flags[3]) {
-        // Some K or V was cleared: the columns that see such a one again, key by key in fp32.  The others keep what they
-        // have.  (Nothing is stored yet: out may be q.)
-        bool again = false;
-        f32x16_t o2[NB];
-        float m2 = -INFINITY, l2 = 0.f;
+    auto store = [&] {
+        const float sum = l + lane_xor(l, 32);
+        const int out_type = TYPE == STAGE_F32 && seq.first + t0 + row < a.pair_rows ? kPair : TYPE;
+        if (row >= rows) return;
+        const size_t to = (size_t)(seq.first + t0 + row) * a.out_ld + at - 8 * half;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o2[b][i] = 0.f;
-#pragma unroll 1
-        for (int i = 0; i < n_tiles * kTileKeys; ++i) {
-            const int key = rb.tile_at(i / kTileKeys) * kTileKeys + i % kTileKeys;
-            if (key / kPage > rb.last_page) continue;
-            const int b = ((const_ints)(uintptr_t)seq.table)[key / kPage];
-            if (!known(b)) continue;
-            const float *const k = pool + (size_t)b * block_elems + key % kPage * D, *const v = k + hkv * head;
-            bool bad = false;
-            float w = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                float x[8], y[8];
-                load4(a.q, q_at + 16 * kk, TYPE, x);
-                load4(a.q, q_at + 16 * kk + 4, TYPE, x + 4);
-                load4(k, 16 * kk + 8 * half, STAGE_F32, y);
-                load4(k, 16 * kk + 8 * half + 4, STAGE_F32, y + 4);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    bad |= !(fabsf(y[j]) <= kMaxBf16);
-                    w = fmaf(x[j], y[j], w);
-                }
-                asm volatile("" ::: "memory");   // (registers)
-            }
-            w = (w + lane_xor(w, 32)) * a.scale * kLog2e;
-            const bool seen = sees(a, pos, key);
-            const float to = seen & (w > m2) ? w : m2, ref = to == -INFINITY ? 0.f : to;
-            const float alpha = __builtin_amdgcn_exp2f(m2 - ref);
-            w = seen ? __builtin_amdgcn_exp2f(w - ref) : 0.f;
-            m2 = to;
-            l2 = l2 * alpha + (half ? 0.f : w);   // (the halves of a column are added up at the end)
-#pragma unroll
-            for (int c = 0; c < NB; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float x[4];
-                    load4(v, 32 * c + 8 * j + 4 * half, STAGE_F32, x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        bad |= !(fabsf(x[e]) <= kMaxBf16);
-                        o2[c][4 * j + e] = o2[c][4 * j + e] * alpha + (seen ? w * x[e] : 0.f);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);   // (registers)
-                }
-            again |= seen & bad;
-        }
-        if (__shfl_xor((int)again, 32) | (int)again) {
-            l = l2;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) o[b] = o2[b];
-        }
-    }
-    const float sum = l + lane_xor(l, 32);
-    const int out_type = TYPE == STAGE_F32 && seq.first + t0 + row < a.pair_rows ? kPair : TYPE;
-    if (row >= rows) return;
-    const size_t to = (size_t)(seq.first + t0 + row) * a.out_ld + at - 8 * half;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            store4(a.out, to + 32 * b + 8 * j + 4 * half, out_type,
-                   quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
+            for (int j = 0; j < 4; ++j)
+                store4(a.out, to + 32 * b + 8 * j + 4 * half, out_type,
+                       quotient(make_float4(o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]), sum));
+    };
+    // Columns that see a K or V that was cleared, or whose sums are not finite, are taken again; the others keep what they
+    // have.  (Rows are stored before, unless out is q, which is read again: behind this rare code all stores came 2 to 5 us later.)
+    const bool same = a.out == a.q;
+    if (!same) store();
+    const bool bad = row < rows && not_finite(l, o);
+    if (lane == 0) flags[wave] = 0;
+    if (odd | bad) flags[wave] = 1;
+    __syncthreads();
+    const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+    if (__builtin_expect(any, 0)) by_keys<D, TYPE, STAGE_F32>(a, rb, g, q_at, pos, bad, o, l);
+    if (__builtin_expect(any | same, 0)) store();
 }
 
 template <int D, int TERMS>

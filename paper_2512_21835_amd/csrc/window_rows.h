@@ -197,6 +197,92 @@ struct RowBlock {
         return w;
     }
 };
+// Numbers by size, those that are not finite from 0x7F800000 on.
+__device__ __forceinline__ uint32_t size_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+// Whether the state of the lane's column holds what is not finite.
+template <int NB>
+__device__ __forceinline__ bool not_finite(float l, const f32x16_t (&o)[NB]) {
+    uint32_t most = size_bits(l);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = max(most, size_bits(o[b][i]));
+    return most >= 0x7F800000u;
+}
+
+// The column of a lane (and of lane ^ 32: d 32 c + 8 j + 4 (lane / 32) + i in o[c][4 j + i]) key by key in fp32, where terms
+// cannot give it: an infinity has none, and 0 x inf in the matrix instructions meets columns that do not see it.  Columns
+// marked `again`, and those that see a K or V that is not finite, or too large to be rounded to bf16; others keep o and l.
+template <int D, int TYPE, int KV_TYPE>
+__device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb, int g, size_t q_at, int pos, bool again, f32x16_t (&o)[D / 32], float &l) {
+    const int half = __lane_id() >> 5;
+    const size_t head = (size_t)kPage * D;
+    auto each_key = [&](auto use) {   // use(key, place of K, place of V), the lane's half of them
+#pragma unroll 1
+        for (int i = 0; i < rb.n_tiles * kTileKeys; ++i) {
+            const int key = rb.tile_at(i / kTileKeys) * kTileKeys + i % kTileKeys;
+            if (key / kPage > rb.last_page) continue;
+            const int b = ((const_ints)(uintptr_t)rb.seq.table)[key / kPage];
+            if ((unsigned)b >= (unsigned)a.rows.n_blocks) continue;
+            const size_t k = ((size_t)b * 2 * a.n_kv_heads + g) * head + key % kPage * D;
+            use(key, k + 8 * half, k + a.n_kv_heads * head + 4 * half);
+        }
+    };
+    each_key([&](int key, size_t k, size_t v) {
+        uint32_t most = 0;
+        float x[4];
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                load4(a.pool, k + c + 4 * h, KV_TYPE, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = max(most, size_bits(x[e]));
+                load4(a.pool, v + c + 8 * h, KV_TYPE, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = max(most, size_bits(x[e]));
+            }
+        again |= sees(a, pos, key) & (most > size_bits(kMaxBf16));
+    });
+    again = __shfl_xor((int)again, 32) | (int)again;
+    float m = -INFINITY;
+    l = again ? 0.f : l;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = again ? 0.f : o[b][i];
+    each_key([&](int key, size_t k, size_t v) {
+        float w = 0.f;
+#pragma unroll 1
+        for (int kk = 0; kk < D / 16; ++kk) {
+            float x[8], y[8];
+            load4(a.q, q_at + 16 * kk, TYPE, x);
+            load4(a.q, q_at + 16 * kk + 4, TYPE, x + 4);
+            load4(a.pool, k + 16 * kk, KV_TYPE, y);
+            load4(a.pool, k + 16 * kk + 4, KV_TYPE, y + 4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w = fmaf(x[j], y[j], w);
+            asm volatile("" ::: "memory");   // (registers)
+        }
+        w = (w + lane_xor(w, 32)) * a.scale * kLog2e;
+        const bool seen = again & sees(a, pos, key);
+        const float to = seen & (w > m) ? w : m, ref = to == -INFINITY ? 0.f : to;
+        const float alpha = again ? __builtin_amdgcn_exp2f(m - ref) : 1.f;
+        w = seen ? __builtin_amdgcn_exp2f(w - ref) : 0.f;
+        m = to;
+        l = l * alpha + (half ? 0.f : w);   // (the halves of a column are added up at the end)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x[4];
+                load4(a.pool, v + 32 * c + 8 * j, KV_TYPE, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[c][4 * j + e] = o[c][4 * j + e] * alpha + (seen ? w * x[e] : 0.f);
+                __builtin_amdgcn_sched_barrier(0);   // (registers)
+            }
+    });
+}
 // With a turn before and a turn behind each run.
 __device__ __forceinline__ Turns widened(Turns w) {
     return {w.low > 0 ? w.low + 1 : 0, w.from - 1, w.n ? w.n + 2 : 0};

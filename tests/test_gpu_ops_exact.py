@@ -101,3 +101,64 @@ def test_window_in_place_with_another_stride_is_refused():
     with pytest.raises(P.StageError) as e:
         P.stage_window_attention(wide[:2], wide[::2], b.pool.cuda(), b.stage_batch(P))
     assert e.value.code == P.STAGE_EINVAL
+
+
+def _poisoned(rows, held, hq, hkv, d, act, cache, what, at, value):
+    """A case, one with |V|, and one in which token 1 of every sequence has `value` in element 9 (or those of `at`) of K or V of
+    KV head 0: a page that prompts behind held tokens see all of."""
+    b, q, out = _window_case(rows, held, hq, hkv, d, act, cache)
+    clean = b.pool.clone()
+    for i in range(len(rows)):
+        if b.lengths[i] > 1:
+            for e, x in zip(at, value):
+                b.pool[int(b.table[i, 0]), what, 0, 1, e] = x
+    return b, q, out, clean
+
+
+def _check_poisoned(b, q, out, clean, window, sinks):
+    got = _run_window((b, q, out), window, sinks).double().cpu()
+    want = O.window(b, q, out, b.pool, q.shape[1], window, sinks)[0]
+    # what the probabilities are off relative to their sums' sizes, as without the odd value; those sizes with it
+    _, off32, off16 = O.window(b, q, out, clean, q.shape[1], window, sinks)
+    sizes = O.window(b, q, out, torch.cat([b.pool[:, :1], b.pool[:, 1:].abs()], 1), q.shape[1], window, sinks)[0]
+    off = sizes * (off32 / (off16 / O.U16) + (2 * 2.0 ** -16 if q.dtype == torch.bfloat16 else 0))
+    odd = ~torch.isfinite(want)
+    assert torch.equal(got[odd], want[odd])
+    O.assert_within(got[~odd], want[~odd], O.rounded(want, off, q.dtype)[~odd])
+    return odd
+
+
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinities_that_rows_see(rows, held, hq, hkv, d, cache, act):
+    """Those of V reach the rows' elements as they are; a key of score -inf drops out."""
+    inf = float("inf")
+    for window, sinks in ((0, 0), (40, 2)):
+        b, q, out, clean = _poisoned(rows, held, hq, hkv, d, act, cache, 1, (9, 10), (inf, -inf))
+        assert bool(_check_poisoned(b, q, out, clean, window, sinks).any())
+        b, q, out, clean = _poisoned(rows, held, hq, hkv, d, act, cache, 0, (9,), (-inf,))
+        q[..., 9] = q[..., 9].abs() + 0.1
+        assert not bool(_check_poisoned(b, q, out, clean, window, sinks).any())
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+@pytest.mark.parametrize("d", [64, 128])
+def test_numbers_too_large_for_bf16(rows, held, hq, hkv, d, cache):
+    """fp32 q and K between the largest bf16 and the largest fp32."""
+    large = 3.4e38
+    b, q, out = c = _window_case(rows, held, hq, hkv, d, "fp32", cache)
+    q[..., 7] = large
+    b.pool[:, 0, :, :, 7] = 2.0 ** -126 * torch.sign(b.pool[:, 0, :, :, 7])
+    got = _run_window(c, 40, 2)
+    want, off32, _ = O.window(b, q, out, b.pool, hq, 40, 2)
+    O.assert_within(got, want, O.rounded(want, off32, torch.float32))
+    if cache == "bf16":
+        return
+    q[..., 7] = 2.0 ** -126
+    b.pool[:, 0, :, :, 7] = large * torch.sign(b.pool[:, 0, :, :, 7])
+    got = _run_window(c, 40, 2)
+    want, off32, _ = O.window(b, q, out, b.pool, hq, 40, 2)
+    O.assert_within(got, want, O.rounded(want, off32, torch.float32))
