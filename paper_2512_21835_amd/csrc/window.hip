@@ -107,8 +107,8 @@ struct Columns {
     }
 
     // The columns whose state is not finite once more, key by key in fp32: of an infinity or a number too large for bf16 the
-    // terms are none (inf - inf).  pool: of the KV head.  (An fp32 cache's products have no terms.)
-    __device__ __forceinline__ void by_keys(const WindowArgs &a, const uint16_t *pool, const int *table, const Span &sp, int beg, int end,
+    // terms are none (inf - inf), and sums of large values pass the largest number.  pool: of the KV head.
+    __device__ __forceinline__ void by_keys(const WindowArgs &a, const char *pool, const int *table, const Span &sp, int beg, int end,
                                             size_t q_at, bool valid) {
         uint32_t most = size_bits(l);
 #pragma unroll
@@ -133,7 +133,7 @@ struct Columns {
             for (int b = 0; b < D / 16; ++b) {
                 float x[4], y[4];
                 load4(a.q, q_at + 16 * b + 4 * lq, a.type, x);
-                load4(pool, k + 16 * b, STAGE_BF16, y);
+                load4(pool, k + 16 * b, F32 ? STAGE_F32 : STAGE_BF16, y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w = fmaf(x[i], y[i], w);
             }
@@ -143,19 +143,19 @@ struct Columns {
             const bool seen = sees(a, pos, key);
             const float to = seen & (w > m2) ? w : m2, ref = to == -INFINITY ? 0.f : to;
             const float alpha = __builtin_amdgcn_exp2f(m2 - ref);
-            w = seen ? __builtin_amdgcn_exp2f(w - ref) : 0.f;
+            w = seen ? __builtin_amdgcn_exp2f(w - ref) * kRoom : 0.f;
             m2 = to;
             l2 = l2 * alpha + (lq == 0 ? w : 0.f);
 #pragma unroll
             for (int b = 0; b < D / 16; ++b) {
                 float x[4];
-                load4(pool, v + 16 * b, STAGE_BF16, x);
+                load4(pool, v + 16 * b, F32 ? STAGE_F32 : STAGE_BF16, x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o2[b][i] = o2[b][i] * alpha + (seen ? w * x[i] : 0.f);
             }
         }
         if (lanes >> (lane & 15) & 0x0001000100010001ull) {
-            m = m2;
+            m = m2 + kRoomBits;
             l = l2;
 #pragma unroll
             for (int b = 0; b < D / 16; ++b) o[b] = o2[b];
@@ -411,8 +411,7 @@ __global__ __launch_bounds__(256) void window_split(WindowArgs a, SplitPlan pl) 
         cols.add(a, ring + u % S * L::BYTES, k0, !all_see(a, first, last, k0, kPage), first, rows);
     }
 
-    if constexpr (!F32)
-        cols.by_keys(a, reinterpret_cast<const uint16_t *>(pool), seq.table, sp, beg, end, row * a.q_ld + (size_t)h * D, t < rows);
+    cols.by_keys(a, pool, seq.table, sp, beg, end, row * a.q_ld + (size_t)h * D, t < rows);
 
     // the wavefronts' states meet in LDS
     float l = cols.l;
@@ -438,7 +437,7 @@ __global__ __launch_bounds__(256) void window_split(WindowArgs a, SplitPlan pl) 
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm[w * 32 + col] - ref);
+            const float f = __builtin_amdgcn_exp2f(sm[w * 32 + col] - ref) * kRoom;
             const f32x4_t v = *reinterpret_cast<const f32x4_t *>(so + (w * 16 + col) * OLD + d);
             sum = fmaf(f, sm[w * 32 + 16 + col], sum);
             o.x = fmaf(f, v.x, o.x);

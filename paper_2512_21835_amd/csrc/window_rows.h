@@ -28,6 +28,9 @@ constexpr long kMaxBlocks = (1L << 24) - 1;   // workgroups of 256 in a grid: th
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;
 constexpr float kMaxBf16 = 0x1.FEp127f;
+// Probabilities and sums of up to 2^24 keys are scaled by this where values near the largest number are added up.
+constexpr int kRoomBits = 24;
+constexpr float kRoom = 1.f / (1 << kRoomBits);
 
 // The same in every lane, and known to be.
 __device__ __forceinline__ OpRows::Seq uniform(OpRows::Seq s) {
@@ -212,7 +215,8 @@ __device__ __forceinline__ bool not_finite(float l, const f32x16_t (&o)[NB]) {
 
 // The column of a lane (and of lane ^ 32: d 32 c + 8 j + 4 (lane / 32) + i in o[c][4 j + i]) key by key in fp32, where terms
 // cannot give it: an infinity has none, and 0 x inf in the matrix instructions meets columns that do not see it.  Columns
-// marked `again`, and those that see a K or V that is not finite, or too large to be rounded to bf16; others keep o and l.
+// marked `again` (sums that pass the largest number among them: scaled by kRoom, they do not), and those that see a K or V
+// that is not finite, or too large to be rounded to bf16; others keep o and l.
 template <int D, int TYPE, int KV_TYPE>
 __device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb, int g, size_t q_at, int pos, bool again, f32x16_t (&o)[D / 32], float &l) {
     const int half = __lane_id() >> 5;
@@ -268,7 +272,7 @@ __device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb,
         const bool seen = again & sees(a, pos, key);
         const float to = seen & (w > m) ? w : m, ref = to == -INFINITY ? 0.f : to;
         const float alpha = again ? __builtin_amdgcn_exp2f(m - ref) : 1.f;
-        w = seen ? __builtin_amdgcn_exp2f(w - ref) : 0.f;
+        w = seen ? __builtin_amdgcn_exp2f(w - ref) * kRoom : 0.f;
         m = to;
         l = l * alpha + (half ? 0.f : w);   // (the halves of a column are added up at the end)
 #pragma unroll

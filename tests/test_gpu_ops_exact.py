@@ -162,3 +162,19 @@ def test_numbers_too_large_for_bf16(rows, held, hq, hkv, d, cache):
     got = _run_window(c, 40, 2)
     want, off32, _ = O.window(b, q, out, b.pool, hq, 40, 2)
     O.assert_within(got, want, O.rounded(want, off32, torch.float32))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_near_the_largest_number(rows, held, hq, hkv, d, cache):
+    """Their mean is one too, though their sum is not."""
+    large = 3.4e38 if cache == "fp32" else 3.3e38
+    b, q, out = c = _window_case(rows, held, hq, hkv, d, "fp32", cache)
+    q[..., 7] = 2.0 ** -126
+    b.pool[:, 0, :, :, 7] = large * torch.sign(b.pool[:, 0, :, :, 7])
+    b.pool[:, 1, :, :, 9] = large
+    for window, sinks in ((40, 2), (0, 0)):
+        got = _run_window(c, window, sinks)
+        want, off32, _ = O.window(b, q, out, b.pool, hq, window, sinks)
+        O.assert_within(got, want, O.rounded(want, off32, torch.float32))
