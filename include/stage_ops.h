@@ -130,7 +130,7 @@ int stage_window_attention(const stage_window_args *a, void *workspace, int64_t 
        out[r] = base[r] + scales[i] * B_i (A_i x[r]),  i = ids[r],
    with the first ranks[i] rows of A_i and columns of B_i (NULL: all max_rank); a row whose id is not in [0, n_adapters)
    has no adapter and becomes base[r].  Sums are in fp32 (A_i x[r] too), the operands of the matrix instructions exact
-   (fp32 ones as sums of bf16 terms); each result is rounded once.  out may be base itself, with the same stride. */
+   (fp32 ones as sums of bf16 terms); each result is rounded once.  Infinities and NaN give what they give in the formula.  out may be base itself, with the same stride. */
 typedef struct {
     int32_t device;
     int32_t rows;

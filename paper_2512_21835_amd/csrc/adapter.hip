@@ -76,6 +76,17 @@ __device__ __forceinline__ void split_terms8(const float v[8], bf16x8_t t[TERMS]
     }
 }
 
+// Whether some are not finite.
+__device__ __forceinline__ bool not_finite(const f32x4_t &v) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return most >= 0x7F800000u;
+}
+
+__device__ __forceinline__ int rank_of(const AdapterArgs &a, int id) {
+    return a.ranks ? min(max(a.ranks[id], 0), a.max_rank) : a.max_rank;
+}
 // The adapters of a tile's rows: lane r < 16 has row r's (-1: none, or of rank 0); `first` has a bit for the first row
 // of each.  Every lane of the wavefront must be active.
 struct TileIds {
@@ -84,7 +95,7 @@ struct TileIds {
     __device__ __forceinline__ void load(const AdapterArgs &a, int row0) {
         const int lane = __lane_id(), row = row0 + (lane & 15);
         id = row < a.rows ? a.ids[row] : -1;
-        rank = (unsigned)id < (unsigned)a.n_adapters ? a.ranks ? min(max(a.ranks[id], 0), a.max_rank) : a.max_rank : 0;
+        rank = (unsigned)id < (unsigned)a.n_adapters ? rank_of(a, id) : 0;
         if (rank == 0) id = -1;
         bool again = id < 0;
 #pragma unroll
@@ -98,6 +109,27 @@ struct AdapterPlan {
     int slices;
     int groups;           // workgroups that share a tile and slice's (adapter, 16 of its ranks) items
 };
+
+// Four of a row's t over n of its k by products of whole numbers: of an infinity, or an x too large for bf16, the terms are
+// none (inf - inf).
+__device__ __forceinline__ f32x4_t whole_sums(const AdapterArgs &a, int row, int id, int j0, int k0, int n) {
+    asm volatile("" : "+v"(id), "+v"(row));   // (nothing of it is worked out ahead, and kept in registers)
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    const uint16_t *const w = a.a + ((size_t)id * a.max_rank + j0) * a.k;
+#pragma unroll 1
+    for (int k = k0; k < min(a.k, k0 + n); k += 8) {
+        float x[8], y[8];
+        if (a.x_pair) load8_pair(a.x, (size_t)row * a.x_ld + pair_at(k), x);
+        else load8(a.x, (size_t)row * a.x_ld + k, STAGE_F32, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            load8(w, (size_t)i * a.k + k, STAGE_BF16, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i] = fmaf(x[j], y[j], v[i]);
+        }
+    }
+    return v;
+}
 
 // t of a tile over a slice of k: a wavefront holds its k of x as operand fragments and takes one item (adapter, 16 of its
 // ranks) after the other, its rows of A copied into LDS one item ahead; the four wavefronts' sums meet in LDS.
@@ -208,10 +240,12 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, Adapte
         wait_lgkm<0>();   // (the copies under way stay so across the barrier)
         lds_barrier();
         // rank 16 jb + 4 lq + i of row l16
-        if (wave == (turn & 3) && t.id == it.id && 16 * it.jb + 4 * lq < a.max_rank) {
+        const int j0 = 16 * it.jb + 4 * lq;
+        if (wave == (turn & 3) && t.id == it.id && j0 < a.max_rank) {
             const f32x4_t *const p = &sums[turn & 1][0][lane];
-            *reinterpret_cast<f32x4_t *>(a.part + ((size_t)slice * a.rows + row0 + l16) * a.max_rank + 16 * it.jb + 4 * lq) =
-                ((p[0] + p[64]) + p[128]) + p[192];
+            f32x4_t v = ((p[0] + p[64]) + p[128]) + p[192];
+            if (__builtin_expect(TERMS > 1 && not_finite(v), 0)) v = whole_sums(a, row0 + l16, it.id, j0, 4 * slice * pl.wave_k, 4 * pl.wave_k);
+            *reinterpret_cast<f32x4_t *>(a.part + ((size_t)slice * a.rows + row0 + l16) * a.max_rank + j0) = v;
         }
         it = after;
     }
@@ -233,6 +267,23 @@ __device__ __forceinline__ u32x4 cut_ranks(u32x4 v, int j0, int rank) {
     for (int j = 0; j < 4; ++j) {
         v[j] = j0 + 2 * j < rank ? v[j] : 0;
         v[j] = j0 + 2 * j + 1 < rank ? v[j] : v[j] & 0xFFFFu;
+    }
+    return v;
+}
+
+// A column of a row's B t, likewise.
+__device__ __forceinline__ float whole_output(const AdapterArgs &a, int slices, int row, int id, int col) {
+    asm volatile("" : "+v"(id), "+v"(row));
+    const int rank = rank_of(a, id);
+    const float scale = a.scales ? a.scales[id] : 1.f;
+    const uint16_t *const w = a.b + ((size_t)id * a.n + col) * a.max_rank;
+    float v = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < rank; ++j) {
+        float t = 0.f;
+#pragma unroll 1
+        for (int s = 0; s < slices; ++s) t += a.part[((size_t)s * a.rows + row) * a.max_rank + j];
+        v = fmaf(t * scale, __uint_as_float((uint32_t)w[j] << 16), v);
     }
     return v;
 }
@@ -487,6 +538,15 @@ __global__ __launch_bounds__(256, T_STEPS * kStep <= kRanks ? 3 : 1) void adapte
             if (any) stores = E;
             const int c0 = kCols * p0.nb + 16 * lq;
             if (write && c0 < a.n) {
+                if (__builtin_expect((t.id >= 0) & (not_finite(sum[0]) | not_finite(sum[1]) | not_finite(sum[2]) | not_finite(sum[3])), 0)) {
+#pragma unroll 1
+                    for (int c = 0; c < 16 && c0 + c < a.n; ++c) {
+                        const float v = whole_output(a, pl.slices, row, t.id, c0 + c);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (i == c && !(fabsf(sum[i / 4][i % 4]) < INFINITY)) sum[i / 4][i % 4] = v;
+                    }
+                }
                 const uint32_t from = y_ring + p0.slot * L::Y_STAGE + l16 * (16 * YCH);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {   // eight columns

@@ -5,7 +5,7 @@ import torch
 
 import paper_2512_21835_amd as P
 from tests import ops_oracle as O
-from tests.test_gpu_ops import _run_window, _window_case
+from tests.test_gpu_ops import _adapter_case, _run_adapter, _run_window, _window_case
 
 pytestmark = pytest.mark.gpu
 
@@ -178,3 +178,50 @@ def test_values_near_the_largest_number(rows, held, hq, hkv, d, cache):
         got = _run_window(c, window, sinks)
         want, off32, _ = O.window(b, q, out, b.pool, hq, window, sinks)
         O.assert_within(got, want, O.rounded(want, off32, torch.float32))
+
+
+# few rows of many adapters (shared out among wavefronts), many rows; ranks of one, some and many MFMA steps; more than eight
+# slices of k
+ADAPTERS = [(16, 520, 200, 5, 12), (5, 264, 1000, 4, 72), (100, 256, 136, 3, 16), (40, 96, 72, 6, 256), (3, 5000, 72, 4, 4)]
+
+
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,k,n,adapters,rank", ADAPTERS)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_adapters_of_infinities(rows, k, n, adapters, rank, act, in_place):
+    """One in x, in A or in B, of an adapter of rank 1 and one of all ranks, reaches what it reaches in the formula."""
+    inf = float("inf")
+    for what in range(3):
+        c = _adapter_case(rows, k, n, adapters, rank, act, [i % adapters for i in range(rows)],
+                          [1 if i == 1 else rank for i in range(adapters)])
+        x, base, a, b = c[:4]
+        for i in (1, 2):
+            if what == 0:
+                x[i, 7] = inf if i == 1 else -inf
+            elif what == 1:
+                a[i, 0, k - 3] = inf
+            else:
+                b[i, 9, 0] = -inf
+        want, off = O.adapter(*c)
+        dev = [t.cuda() for t in c]
+        out = dev[1] if in_place else torch.empty_like(dev[1])
+        got = P.stage_adapter_add(dev[0], dev[1], out, *dev[2:]).double().cpu()
+        odd = ~torch.isfinite(want)
+        assert bool(odd.any()) and torch.equal(torch.isnan(got), torch.isnan(want))
+        assert torch.equal(torch.nan_to_num(got[odd]), torch.nan_to_num(want.to(x.dtype)[odd].double()))
+        O.assert_within(got[~odd], want[~odd], O.rounded(want, off, x.dtype)[~odd])
+
+
+@pytest.mark.parametrize("rows,k,n,adapters,rank", ADAPTERS)
+def test_adapters_of_numbers_too_large_for_bf16(rows, k, n, adapters, rank):
+    """fp32 x and A x between the largest bf16 and the largest fp32."""
+    c = _adapter_case(rows, k, n, adapters, rank, "fp32", [i % adapters for i in range(rows)])
+    c[0][:, 3] = 3.4e38
+    c[2][..., 3] = 2.0 ** -126 * torch.sign(c[2][..., 3])
+    want, off = O.adapter(*c)
+    O.assert_within(_run_adapter(c), want, O.rounded(want, off, torch.float32))
+    c[2].zero_()
+    c[2][:, 0, 3] = 1.0                    # t 3.4e38
+    c[3][..., 0] = 2.0 ** -126 * torch.sign(c[3][..., 0])
+    want, off = O.adapter(*c[:6], torch.ones(adapters))
+    O.assert_within(_run_adapter((*c[:6], None)), want, O.rounded(want, off, torch.float32))
