@@ -12,7 +12,8 @@
  *    block ids, positions, adapter ids) is checked by the kernels, which leave out what is out of range
  *    as each function states, so no value of theirs is read or written out of bounds.
  *  - Work is enqueued on `stream` (a hipStream_t of `device`; NULL: its null stream) and the call returns before
- *    it runs.  Nothing is allocated and nothing waits, so calls may be captured into a HIP graph.  Calls
+ *    it runs; its buffers, workspace among them, must stay until then.  Nothing is allocated and nothing waits, so calls may be
+ *    captured into a HIP graph.  Calls
  *    may run at once on several streams and host threads if they share no output and no workspace.
  *  - Row strides (*_ld) are in elements.  Rows start on 16-byte boundaries: pointers and row strides in
  *    bytes are multiples of 16 (EINVAL otherwise).

@@ -2,8 +2,9 @@
 
 Argument marshalling and the checks that need the tensors' shapes; the library checks the rest.  A call
 runs on the current torch stream of its tensors' device unless ``stream`` (a torch stream of it) is given,
-and returns the tensor that it writes.  Where a call needs a workspace and none is given, one is taken
-from torch's allocator, on that stream.
+and returns the tensor that it writes.  With ``stream`` the tensors' memory is kept until the call is done there, as by
+Tensor.record_stream; waiting for their contents is the caller's.  Where a call needs a workspace and none is given, one is
+taken from torch's allocator, on that stream.
 """
 from __future__ import annotations
 
@@ -137,6 +138,14 @@ def _handle(stream, device: int) -> int:
     return stream.cuda_stream
 
 
+def _keep(stream, *tensors: Optional[torch.Tensor]) -> None:
+    """The tensors' memory goes to nobody else before what is enqueued on `stream` is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _current_stream(device: int) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
@@ -191,6 +200,7 @@ def stage_norm_rope_append(qkv: torch.Tensor, q_out: torch.Tensor, pool: torch.T
         rc = lib().stage_norm_rope_append(args, _handle(stream, device))
         if rc:
             _check(rc)
+        _keep(stream, qkv, q_out, pool, cos, sin, q_gain, k_gain, positions, *batch.tensors)
     return q_out
 
 
@@ -224,6 +234,7 @@ def stage_window_attention(q: torch.Tensor, out: torch.Tensor, pool: torch.Tenso
         rc = L.stage_window_attention(args, ws, size, _handle(stream, device))
         if rc:
             _check(rc)
+        _keep(stream, q, out, pool, workspace, *batch.tensors)
     return out
 
 
@@ -262,4 +273,5 @@ def stage_adapter_add(x: torch.Tensor, base: torch.Tensor, out: torch.Tensor, a:
         rc = L.stage_adapter_add(args, ws, size, _handle(stream, device))
         if rc:
             _check(rc)
+        _keep(stream, x, base, out, a, b, ids, ranks, scales, workspace)
     return out
