@@ -40,7 +40,7 @@ extern "C" {
 #define STAGE_OPS_MAX_RANK 256
 
 /* The sequences of a call and their rows.  Sequence i owns rows row_start[i] .. row_start[i + 1] - 1 of the
-   call's buffers and holds length[i] tokens once they are counted in: its row t sits at position length[i]
+   call's buffers and holds length[i] tokens (0 to 2^30) once they are counted in: its row t sits at position length[i]
    - (row_start[i + 1] - row_start[i]) + t.  A sequence may have no row.  row_start ascends from 0; rows from
    row_start[n_seqs] on are padding, which no function reads or writes.  Position p is in block block_table[i][p / 16],
    place p % 16. */

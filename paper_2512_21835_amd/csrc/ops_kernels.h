@@ -12,6 +12,9 @@
 
 namespace stg {
 
+// Lengths of a caller's sequences count as this at most, and as 0 at least: no sum or difference of theirs overflows.
+constexpr int kMaxLength = 1 << 30;
+
 // The rows of a call and the cache places of their sequences: the caller's batch (row_start), or the
 // equal rows per sequence of a stage call (rows_per_seq of map, its row metadata).  What a kernel takes from device
 // memory is clamped here or checked by it: no value of the caller's leads out of a buffer.
@@ -31,7 +34,7 @@ struct OpRows {
         if (!row_start)
             return {i * map.rows_per_seq, map.rows_per_seq, map.pos0(i), table + (size_t)map.seq_slot(i) * max_blocks};
         const int b = min(max(row_start[i], 0), rows), e = min(max(row_start[i + 1], b), rows);
-        return {b, e - b, length[i] - (e - b), table + (size_t)i * max_blocks};
+        return {b, e - b, min(max(length[i], 0), kMaxLength) - (e - b), table + (size_t)i * max_blocks};
     }
     // The sequence of a row: how many of row_start[1 ..] are not above it.  n_seqs for a row of padding.  One load
     // per lane, so that up to 64 sequences cost one round trip; every lane of the wavefront must be active and

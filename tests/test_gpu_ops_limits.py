@@ -1,0 +1,48 @@
+"""Sequences past a call's max_len and max_rows, row starts and lengths out of order."""
+import copy
+
+import pytest
+import torch
+
+import paper_2512_21835_amd as P
+from tests import ops_oracle as O
+from tests.test_gpu_ops import _append_case, _check_append, _run_append, _run_window, _window_case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (72, 9)])
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+def test_window_of_more_rows_than_max_rows(hq, hkv, cache):
+    """The rows beyond keep what out holds; the others are as with all of them."""
+    b, q, out = c = _window_case([37, 1, 70, 30], [30, 60, 200, 0], hq, hkv, 64, "fp32", cache)
+    b.max_rows = 32
+    got = _run_window(c, 40, 2)
+    want, off32, _ = O.window(b, q, out, b.pool, hq, 40, 2)
+    for i, n in enumerate(b.rows):
+        at = int(b.start[i])
+        want[at + 32:at + n], off32[at + 32:at + n] = out[at + 32:at + n], 0
+        assert torch.equal(got[at + 32:at + n].cpu(), out[at + 32:at + n])
+    O.assert_within(got, want, O.rounded(want, off32, torch.float32))
+
+
+def test_append_past_max_len():
+    c = _append_case([20, 6, 40], [10, 60, 20], 4, 2, 64)
+    c[0].max_len = 48
+    _check_append(c, *_run_append(c))
+
+
+@pytest.mark.parametrize("length", [-1, -5, -(1 << 31), -(1 << 31) + 3])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (72, 9)])
+def test_lengths_below_zero_hold_nothing(length, hq, hkv):
+    b, q, out = c = _window_case([30, 40, 60], [20, 0, 33], hq, hkv, 64, "fp32", "bf16")
+    b.lengths[1] = 0                           # (the oracle: as many tokens)
+    b.length[1] = length
+    got = _run_window(c, 0, 16)
+    want, off32, _ = O.window(b, q, out, b.pool, hq, 0, 16)
+    assert not bool(got[30:70].any())
+    O.assert_within(got, want, O.rounded(want, off32, torch.float32))
+    c = _append_case([30, 40, 60], [20, 0, 33], 8, 2, 64)
+    c[0].lengths[1] = 0
+    c[0].length[1] = length
+    _check_append(c, *_run_append(c))
