@@ -81,8 +81,8 @@ WindowArgs window_args(const stage_window_args &a, void *workspace) {
     w.n_kv_heads = a.cache.n_kv_heads;
     w.head_dim = a.cache.head_dim;
     w.kv_type = a.cache.type;
-    // (no window, or one beyond the longest sequence: every earlier position; sinks likewise)
-    w.window = a.window == 0 || a.window > a.batch.max_len ? a.batch.max_len : a.window;
+    // (no window: one beyond every position, which sequences of more than max_len tokens have as well)
+    w.window = a.window == 0 || a.window > kMaxLength ? kMaxLength : a.window;
     w.sinks = a.sinks > a.batch.max_len ? a.batch.max_len : a.sinks;
     w.scale = a.scale == 0.f ? 1.f / std::sqrt((float)a.cache.head_dim) : a.scale;
     w.part = static_cast<float *>(workspace);

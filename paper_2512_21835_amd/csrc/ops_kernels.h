@@ -12,7 +12,7 @@
 
 namespace stg {
 
-// Lengths of a caller's sequences count as this at most, and as 0 at least: no sum or difference of theirs overflows.
+// Lengths of a caller's sequences, and windows, count as this at most (lengths as 0 at least): no sum or difference of theirs overflows.
 constexpr int kMaxLength = 1 << 30;
 
 // The rows of a call and the cache places of their sequences: the caller's batch (row_start), or the

@@ -11,6 +11,25 @@ from tests.test_gpu_ops import _append_case, _check_append, _run_append, _run_wi
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("cache", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,held,hq,hkv", [([1, 1, 1], [60, 300, 20], 8, 2), ([37, 1, 70, 30], [30, 60, 200, 0], 8, 2),
+                                              ([37, 1, 70, 30], [30, 60, 200, 0], 72, 9)])
+def test_window_of_sequences_past_max_len(rows, held, hq, hkv, cache, act):
+    """Tokens from max_len on are not seen, by rows of positions past it neither; a window of 0 or beyond max_len still
+    reaches back to the first token."""
+    b, q, out = c = _window_case(rows, held, hq, hkv, 64, act, cache)
+    b.max_len = 48
+    seen = copy.copy(b)
+    seen.table = b.table.clone()
+    seen.table[:, 3:] = -7                     # the oracle: blocks that lead nowhere
+    for window, sinks in ((0, 0), (60, 0), (100, 3), (20, 5), (1 << 30, 0), ((1 << 31) - 1, 2)):
+        got = _run_window(c, window, sinks)
+        want, off32, off16 = O.window(seen, q, out, b.pool, hq, window, sinks)
+        off = off32 + off16 if act == "bf16" else off32
+        O.assert_within(got, want, O.rounded(want, off, q.dtype), (window, sinks))
+
+
 @pytest.mark.parametrize("hq,hkv", [(8, 2), (72, 9)])
 @pytest.mark.parametrize("cache", ["bf16", "fp32"])
 def test_window_of_more_rows_than_max_rows(hq, hkv, cache):
