@@ -1643,7 +1643,7 @@ int stage_init(const stage_config *cfg, stage **out) {
     const bool ops_ok = !ops || ((c.head_norm == 0 || c.head_norm == 1) && c.window >= 0 && c.sinks >= 0 &&
                                  (c.window > 0 || c.sinks == 0) && (c.max_adapters > 0) == (c.adapter_rank > 0) &&
                                  c.max_adapters >= 0 && c.max_adapters <= kMaxAdapters &&
-                                 c.adapter_rank <= STAGE_OPS_MAX_RANK && c.adapter_rank % 4 == 0 &&
+                                 c.adapter_rank >= 0 && c.adapter_rank <= STAGE_OPS_MAX_RANK && c.adapter_rank % 4 == 0 &&
                                  (c.head_dim == 64 || c.head_dim == 128) && group <= 8 && (group & (group - 1)) == 0);
     if (!shape_ok || !cap_ok || !ops_ok) return STAGE_EINVAL;
     if (c.plan_mode != 0 && c.plan_mode != 1) return STAGE_EINVAL;
