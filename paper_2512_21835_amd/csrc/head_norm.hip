@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     if (i >= a.rows.n_seqs) return;   // padding
     const OpRows::Seq s = a.rows.seq(i);
     const int place = row - s.first, pos = s.pos0 + place;
-    if (place >= a.rows.max_rows || pos < 0 || pos >= a.rows.max_len) return;
+    if ((unsigned)place >= (unsigned)a.rows.max_rows || pos < 0 || pos >= a.rows.max_len) return;
     const int block = s.table[pos / kBlockTokens];
     if ((unsigned)block >= (unsigned)a.rows.n_blocks) return;
     int at[3] = {pos, pos, pos};

@@ -65,3 +65,20 @@ def test_lengths_below_zero_hold_nothing(length, hq, hkv):
     c[0].lengths[1] = 0
     c[0].length[1] = length
     _check_append(c, *_run_append(c))
+
+
+def test_rows_before_the_first_row_start_are_nobodys():
+    """row_start from 3: the rows before it, as those behind the last, change nothing."""
+    b, qkv, q, cos, sin, gains, _, _, eps = _append_case([5, 4], [12, 30], 8, 2, 64, pad=3)
+    b.start = b.start + 3
+    got, pool = q.cuda(), b.pool.cuda()
+    P.stage_norm_rope_append(qkv.cuda(), got, pool, b.stage_batch(P), cos.cuda(), sin.cuda(), gains[0].cuda(), gains[1].cuda(), eps)
+    want_q, want_kv, off_q, off_kv = O.append(b, qkv[3:], q[3:], b.pool, cos, sin, 8, *gains, eps)
+    assert torch.equal(got[:3].cpu(), q[:3])
+    O.assert_within(got[3:], want_q, O.rounded(want_q, off_q, torch.float32), "q")
+    O.assert_within(pool, want_kv, O.rounded(want_kv, off_kv, torch.bfloat16) * (off_kv > 0) + (off_kv == 0) * want_kv.abs() * O.U16, "pool")
+    kept = (off_kv == 0) & (want_kv == b.pool.double())
+    assert torch.equal(pool.cpu()[kept], b.pool[kept])
+    out = q.cuda()
+    P.stage_window_attention(got, out, pool, b.stage_batch(P), window=20)
+    assert torch.equal(out[:3].cpu(), q[:3])
