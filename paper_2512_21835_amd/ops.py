@@ -4,7 +4,8 @@ Argument marshalling and the checks that need the tensors' shapes; the library c
 runs on the current torch stream of its tensors' device unless ``stream`` (a torch stream of it) is given,
 and returns the tensor that it writes.  With ``stream`` the tensors' memory is kept until the call is done there, as by
 Tensor.record_stream; waiting for their contents is the caller's.  Where a call needs a workspace and none is given, one is
-taken from torch's allocator, on that stream.
+taken from torch's allocator, on that stream.  The operators have no backward pass: where gradients are being recorded,
+tensors that require one are refused.
 """
 from __future__ import annotations
 
@@ -58,6 +59,13 @@ _BATCH = struct.Struct("@iiiiPPP")
 _APPEND = struct.Struct("@i4x40sPiiii ii PP qq ii PP fi PPP iiii")
 _WINDOW = struct.Struct("@i4x40sPiiii ii iif4x PP qq i4x")
 _ADAPTER = struct.Struct("@iiiiiii4x PPP qqq PPP PP")
+
+
+_recording = torch.is_grad_enabled
+
+
+def _no_backward() -> ValueError:
+    return ValueError("the operators have no backward pass: a tensor that requires a gradient is taken under torch.no_grad() only")
 
 
 def _device(t: torch.Tensor) -> int:
@@ -175,6 +183,9 @@ def stage_norm_rope_append(qkv: torch.Tensor, q_out: torch.Tensor, pool: torch.T
                            stream=None) -> torch.Tensor:
     """Norm of the query and key heads of qkv [rows, Hq + 2 Hkv, d], rotation, append to pool; queries to q_out [rows, Hq,
     d].  positions int32 [rows], or [3, rows] with the pairs per axis in ``sections``."""
+    if _recording() and (qkv.requires_grad or q_out.requires_grad or pool.requires_grad or cos.requires_grad or sin.requires_grad or
+                         (q_gain is not None and q_gain.requires_grad) or (k_gain is not None and k_gain.requires_grad)):
+        raise _no_backward()
     device = _device(qkv)
     cache = _cache(pool, device)
     d, hkv = cache[3], cache[2]
@@ -205,6 +216,8 @@ def stage_norm_rope_append(qkv: torch.Tensor, q_out: torch.Tensor, pool: torch.T
 
 
 def _window_args(q, out, pool, batch, window, sinks, scale):
+    if _recording() and (q.requires_grad or out.requires_grad or pool.requires_grad):
+        raise _no_backward()
     device = _device(q)
     cache = _cache(pool, device)
     shape = q.shape
@@ -239,6 +252,9 @@ def stage_window_attention(q: torch.Tensor, out: torch.Tensor, pool: torch.Tenso
 
 
 def _adapter_args(x, base, out, a, b, ids, ranks, scales):
+    if _recording() and (x.requires_grad or base.requires_grad or out.requires_grad or a.requires_grad or b.requires_grad or
+                         (scales is not None and scales.requires_grad)):
+        raise _no_backward()
     device = _device(x)
     if x.dim() != 2 or base.dim() != 2 or base.shape != out.shape or base.shape[0] != x.shape[0] or \
             not x.dtype is base.dtype is out.dtype or a.dim() != 3:
