@@ -5,7 +5,7 @@ import torch
 
 import paper_2512_21835_amd as P
 from tests import ops_oracle as O
-from tests.test_gpu_ops import _adapter_case, _run_adapter, _run_window, _window_case
+from tests.test_gpu_ops import _adapter_case, _check_adapter, _run_adapter, _run_window, _window_case
 
 pytestmark = pytest.mark.gpu
 
@@ -225,3 +225,13 @@ def test_adapters_of_numbers_too_large_for_bf16(rows, k, n, adapters, rank):
     c[3][..., 0] = 2.0 ** -126 * torch.sign(c[3][..., 0])
     want, off = O.adapter(*c[:6], torch.ones(adapters))
     O.assert_within(_run_adapter((*c[:6], None)), want, O.rounded(want, off, torch.float32))
+
+
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,k,n,adapters,rank", ADAPTERS + [(16, 8200, 4096, 8, 128), (33, 9000, 264, 16, 200), (1, 4104, 8, 4, 68)])
+def test_adapters_of_many_ranks_and_slices(rows, k, n, adapters, rank, act):
+    ids = [i * 7 % (adapters + 1) - 1 for i in range(rows)]
+    ranks = [max(1, rank - 13 * i) for i in range(adapters)]
+    _check_adapter(_adapter_case(rows, k, n, adapters, rank, act, ids), _run_adapter(_adapter_case(rows, k, n, adapters, rank, act, ids)))
+    c = _adapter_case(rows, k, n, adapters, rank, act, ids, ranks)
+    _check_adapter(c, _run_adapter(c))
