@@ -497,6 +497,14 @@ __global__ __launch_bounds__(256) void window_merge(WindowArgs a, SplitPlan pl) 
     if (sl == 0) store4(a.out, row * a.out_ld + (size_t)h * D + 4 * cg, (long)row < a.pair_rows ? kPair : a.type, quotient(o, l));
 }
 
+// Blocks of `columns` columns that a call's rows fill, at most: of equal sequences, or no sequence adding more than one that is
+// not full.
+long row_blocks(const WindowArgs &a, long columns) {
+    const long bq = columns * a.n_kv_heads / a.n_q_heads, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
+    const long equal = (long)a.rows.n_seqs * ((a.rows.max_rows + bq - 1) / bq), ragged = a.rows.rows / bq + seqs;
+    return (equal < ragged ? equal : ragged) * a.n_kv_heads;
+}
+
 SplitPlan split_plan(const WindowArgs &a) {
     SplitPlan p{};
     while (a.n_kv_heads << p.log_g < a.n_q_heads) ++p.log_g;
@@ -506,10 +514,7 @@ SplitPlan split_plan(const WindowArgs &a) {
     const long all = (a.rows.max_len + kPage - 1) / kPage;
     const long listed = (a.sinks + kPage - 1) / kPage + ((long)a.window + bq + 2 * kPage - 3) / kPage;
     const long pages = listed < all ? listed : all;
-    // (of a sequence, no more than of the longest; of all, no sequence adds more than one that is not full)
-    const long seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
-    const long equal = (long)a.rows.n_seqs * ((most + bq - 1) / bq), ragged = a.rows.rows / bq + seqs;
-    const long blocks = (p.one_block || equal < ragged ? equal : ragged) * a.n_kv_heads;
+    const long blocks = p.one_block ? (long)a.rows.n_seqs * a.n_kv_heads : row_blocks(a, 16);
     p.blocks = blocks > kMaxBlocks ? 0 : (int)blocks;
     // Workgroups that run at once: 128 KB of LDS each, 64 KB with bf16 heads of 64.  As many splits as fill one to four
     // rounds of them, whichever ends first: a round takes a wavefront's pages and the time of three to begin and end, the
@@ -908,16 +913,27 @@ hipError_t launch_tiles(const WindowArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Whether a call's rows go 128 columns to a workgroup (each of which walks all keys that they see) or 16, the keys cut.
-// A workgroup of 128 takes as long for a tile of keys as a compute unit takes for 2 of 16 columns (bf16: 0.82 and
-// 0.40 us, fp32 cache and rows: 3.6 and 1.24 us); what counts are rounds of the one over the compute units, and those
-// of the other, which keep all of them busy.  64 heads of 8 groups, bf16, split and tiles: 1 sequence of 20 rows behind
-// 4096 tokens 54 and 108 us, 8 of them 184 and 116 us, 4 of 512 rows 1811 and 289 us.
+// Whether a call's rows go 128 columns to a workgroup (each of which walks all keys that they see) or 16, the keys cut: the
+// one that takes less time for the longest list, in us.  Tiles: 8, and for each round of workgroups over the compute units 1 and
+// `tile` for 32 keys.  Split: 12, 5 (2) for each round that it could fill, `keys` for 32 keys of a workgroup, shared by all units,
+// and 0.1 for 32 keys at all.  (Measured: 245 shapes of 1 to 32 sequences of 17 to 1500 rows, 2 to 40 KV heads, lists of up to
+// 5500 keys, types as below.  The kernel taken is 0.5% above the better on the mean, at most 1.31 times; by counts of blocks
+// alone it was 10%, up to 3.6 times.)  64 heads of 8 groups, bf16, tiles and split: 1 sequence of 64 rows 9 and 23 us, behind
+// 4000 tokens 147 and 77, 16 of 17 rows behind them 177 and 318.
 bool by_tiles(const WindowArgs &a) {
-    const long g = a.n_q_heads / a.n_kv_heads, seqs = a.rows.n_seqs < a.rows.rows ? a.rows.n_seqs : a.rows.rows;
-    const long small = (a.rows.rows * g / 16 + seqs) * a.n_kv_heads, large = (a.rows.rows * g / 128 + seqs) * a.n_kv_heads;
-    const long units = device_compute_units();
-    return a.rows.max_rows * g > 16 && small > 2 * units * ((large + units - 1) / units);
+    if (a.rows.max_rows * (long)(a.n_q_heads / a.n_kv_heads) <= 16) return false;
+    const bool f32 = a.kv_type == STAGE_F32, exact = a.type == STAGE_F32, wide = a.head_dim == 128;
+    const double tile = (f32 ? exact ? 2.4 : 1.75 : exact ? 1.3 : 0.9) * (wide ? 1. : 0.67);
+    const double keys = f32 ? wide ? 0.9 : 0.57 : wide ? 0.45 : 0.2, round = f32 || wide ? 5. : 2.;
+    const long units = device_compute_units(), small = row_blocks(a, 16), large = row_blocks(a, 128);
+    auto list = [&](long columns) {   // in tiles
+        const long bq = columns * a.n_kv_heads / a.n_q_heads, all = (a.rows.max_len + kTileKeys - 1) / kTileKeys;
+        const long listed = (a.sinks + kTileKeys - 1) / kTileKeys + ((long)a.window + bq + 2 * kTileKeys - 3) / kTileKeys;
+        return (double)(listed < all ? listed : all);
+    };
+    const double tiles = 8 + (double)((large + units - 1) / units) * (1 + tile * list(128));
+    const double split = 12 + (double)((small + units - 1) / units) * round + list(16) * (keys * (double)small / (double)units + 0.1);
+    return tiles < split;
 }
 
 }  // namespace
