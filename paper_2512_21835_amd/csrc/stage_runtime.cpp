@@ -175,6 +175,7 @@ struct stage {
     size_t ops_bytes = 0;
     int max_ctx = 0;          // longest sequence of the call in flight
     std::vector<int> adapter_of;   // per sequence (-1: none)
+    std::vector<int> call_adapters;   // those that sequences of the call in flight have
     void *ws_dense = nullptr;
     size_t ws_dense_bytes = 0;
 
@@ -676,10 +677,18 @@ int ensure_ops(stage *s, int rows, int T) {
     return STAGE_OK;
 }
 
+// Whether some sequence of the call has an adapter that is set for this projection.
+bool adapted(const stage *s, int layer, int target) {
+    const Adapters &d = s->layers[layer].adapters[target];
+    if (d.n_set == 0) return false;
+    for (int id : s->call_adapters)
+        if (d.set[id] > 0) return true;
+    return false;
+}
 // out += what the rows' adapters of a projection add (x: fp32 rows or the pair of a GEMM operand).
 int run_adapters(stage *s, int layer, int target, int rows, const void *x, long x_ld, bool x_pair, float *out) {
+    if (!adapted(s, layer, target)) return STAGE_OK;
     const Adapters &d = s->layers[layer].adapters[target];
-    if (d.n_set == 0) return STAGE_OK;
     AdapterArgs a = adapter_args(s, target, rows);
     a.x = x;
     a.x_ld = x_ld;
@@ -1290,7 +1299,7 @@ int run_layer_kernels(stage *s, int layer, const LayerWeights &w, int rows, int 
         g.q.out = s->ws_qkv;
         g.q.out_ld = s->qkv_rows;
         HIP_TRY(launch_gemv(GEMV_NORM_STORE, g.q, s->cs));
-        if (s->layers[layer].adapters[STAGE_ADAPT_QKV].n_set) {   // (the GEMV keeps the normalised input to itself)
+        if (adapted(s, layer, STAGE_ADAPT_QKV)) {   // (the GEMV keeps the normalised input to itself)
             HIP_TRY(launch_rmsnorm_split(x_src, g.q.gain, s->cfg.rms_eps, rows, s->H, s->ws_pair, pair_ld(s->H), s->cs));
             if ((rc = run_adapters(s, layer, STAGE_ADAPT_QKV, rows, s->ws_pair, pair_ld(s->H), true, s->ws_qkv))) return rc;
         }
@@ -1470,11 +1479,13 @@ int run_call_body(stage *s, int n_mb, const int32_t *mb_ids, int B, int T, const
     }
     const RowMap row_map{meta.n_seqs > 1 ? s->d_meta : nullptr, T, meta.seq_slot[0], meta.pos0[0]};
     if (row_map.seqs) HIP_TRY(launch_meta_write(meta, s->d_meta, s->cs));
-    if (c.max_adapters) {
-        SeqAdapters of{};
-        for (size_t i = 0; i < slots.size(); ++i) of.id[i] = s->adapter_of[slots[i]];
-        HIP_TRY(launch_adapter_rows(of, (int)rows, T, static_cast<int *>(s->ws_ops), s->cs));
+    s->call_adapters.clear();
+    SeqAdapters of{};
+    for (size_t i = 0; i < slots.size() && c.max_adapters; ++i) {
+        of.id[i] = s->adapter_of[slots[i]];
+        if (of.id[i] >= 0) s->call_adapters.push_back(of.id[i]);
     }
+    if (!s->call_adapters.empty()) HIP_TRY(launch_adapter_rows(of, (int)rows, T, static_cast<int *>(s->ws_ops), s->cs));
     s->calls++;
     if (decode) s->tok_decode += (long long)rows; else s->tok_prefill += (long long)rows;
 
@@ -1694,6 +1705,7 @@ int stage_init(const stage_config *cfg, stage **out) {
     s->lengths.assign(s->n_seq_slots, 0);
     s->parked.assign(s->n_seq_slots, 0);
     s->adapter_of.assign(s->n_seq_slots, -1);
+    s->call_adapters.reserve(kMaxSeqs);
     s->park_host.assign(s->n_seq_slots, nullptr);
     s->park_host_dev.assign(s->n_seq_slots, nullptr);
     s->ready_ev.assign(s->n_seq_slots, nullptr);
