@@ -12,9 +12,9 @@
  *    block ids, positions, adapter ids) is checked by the kernels, which leave out what is out of range
  *    as each function states, so no value of theirs is read or written out of bounds.
  *  - Work is enqueued on `stream` (a hipStream_t of `device`; NULL: its null stream) and the call returns before
- *    it runs; its buffers, workspace among them, must stay until then.  Nothing is allocated and nothing waits, so calls may be
- *    captured into a HIP graph.  Calls
- *    may run at once on several streams and host threads if they share no output and no workspace.
+ *    it runs; its buffers, workspace among them, must stay until then.  Nothing is allocated and nothing waits, so
+ *    calls may be captured into a HIP graph.  Calls may run at once on several streams and host threads if they share
+ *    no output and no workspace.
  *  - Row strides (*_ld) are in elements.  Rows start on 16-byte boundaries: pointers and row strides in
  *    bytes are multiples of 16 (EINVAL otherwise).
  *  - EINVAL: a size, type, stride or pointer that the function does not take; ENOMEM: the workspace is
@@ -41,9 +41,9 @@ extern "C" {
 
 /* The sequences of a call and their rows.  Sequence i owns rows row_start[i] .. row_start[i + 1] - 1 of the
    call's buffers and holds length[i] tokens (0 to 2^30) once they are counted in: its row t sits at position length[i]
-   - (row_start[i + 1] - row_start[i]) + t.  A sequence may have no row.  row_start ascends from 0; rows from
-   row_start[n_seqs] on are padding, which no function reads or writes.  Position p is in block block_table[i][p / 16],
-   place p % 16. */
+   - (row_start[i + 1] - row_start[i]) + t.  A sequence may have no row.  row_start ascends; rows before row_start[0] and
+   from row_start[n_seqs] on are padding, which no function writes and no result depends on.  Position p is in block
+   block_table[i][p / 16], place p % 16. */
 typedef struct {
     int32_t n_seqs;
     int32_t max_rows;   /* no sequence has more rows (rows beyond are left out) */
@@ -76,8 +76,9 @@ typedef struct {
    (height), the last section[2] the third (width), for images and video; n_axes 1: section[0] is head_dim / 2.
 
    A row is left out (q_out and the cache keep what they hold) if its position is negative, not below max_len, or its
-   block id is not one of the pool's, or if an angle's position is not in [0, n_angles).  Two rows of a call
-   must not name the same place of the cache.  q_out may be qkv itself, with the same type and stride. */
+   block id is not one of the pool's, or if an angle's position is not in [0, n_angles); positions of an axis without
+   pairs do not matter.  Two rows of a call must not name the same place of the cache.  q_out may be qkv itself, with the
+   same type and stride. */
 typedef struct {
     int32_t device;
     stage_batch batch;
@@ -106,8 +107,9 @@ int stage_norm_rope_append(const stage_append_args *a, void *stream);
    activations the probabilities, and the values of an fp32 cache, may be held to 2^-16 of their sizes.  Nothing of
    a place that a row does not see reaches its result, infinities and NaN among it; those that it sees give what they give
    in the formula.  Tokens in blocks whose id is not one of the pool's are not seen; a row that sees none (its position is
-   negative, say) becomes 0.  out may be q itself, with
-   the same stride; else they share no element. */
+   negative, say) becomes 0.  out may be q itself, with the same stride; else they share no element.  The order in which a
+   row's keys are added up goes by the call's sizes (rows, sequences, longest length): the same call gives the same bits,
+   the same row in another call the same to rounding. */
 typedef struct {
     int32_t device;
     stage_batch batch;

@@ -72,9 +72,10 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     if ((unsigned)block >= (unsigned)a.rows.n_blocks) return;
     int at[3] = {pos, pos, pos};
     if (a.positions) {
-        at[0] = a.positions[row];
-        at[1] = a.axis1 < HALF ? a.positions[a.rows.rows + row] : at[0];
-        at[2] = a.axis2 < HALF ? a.positions[2 * (size_t)a.rows.rows + row] : at[0];
+        // (an axis without pairs turns nothing by its position)
+        at[0] = a.axis1 > 0 ? a.positions[row] : 0;
+        at[1] = a.axis1 < a.axis2 ? a.positions[a.rows.rows + row] : 0;
+        at[2] = a.axis2 < HALF ? a.positions[2 * (size_t)a.rows.rows + row] : 0;
     }
     for (int x : at)
         if ((unsigned)x >= (unsigned)a.n_angles) return;

@@ -82,3 +82,16 @@ def test_rows_before_the_first_row_start_are_nobodys():
     out = q.cuda()
     P.stage_window_attention(got, out, pool, b.stage_batch(P), window=20)
     assert torch.equal(out[:3].cpu(), q[:3])
+
+
+@pytest.mark.parametrize("sections", [(0, 32, 0), (0, 0, 32), (32, 0, 0), (0, 5, 27), (7, 0, 25), (12, 20, 0)])
+def test_positions_of_axes_without_pairs_do_not_matter(sections):
+    c = list(_append_case([6, 5], [3, 30], 8, 4, 64, axes=3))
+    c[7] = list(sections)
+    want = _run_append(c)
+    _check_append(c, *want)
+    for axis, n in enumerate(sections):
+        if n == 0:
+            c[6][axis] = torch.tensor([-1, 1 << 30] * 6)[:11]
+    got = _run_append(c)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
