@@ -1,12 +1,13 @@
 """What a stage's operator fields refuse, beside tests/test_gpu_stage_ops.py."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2512_21835_amd as P
 from tests import harness
-from tests.test_gpu_stage_ops import SHAPES, TARGETS, Model
+from tests.test_gpu_stage_ops import FEATURES, IDS, SHAPES, TARGETS, Model, _check
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,35 @@ def test_a_call_without_adapters_launches_none(B, head_norm):
     assert torch.equal(*outs)
     assert plain == none < one < two
     assert unset <= plain + 1                # (that a sequence has one is told to the device)
+
+
+@pytest.mark.parametrize("kv_fp32", [False, True])
+def test_micro_batches_of_one_call_or_one_by_one(kv_fp32):
+    """A window's keys may be added up in another order: both groupings are held to the float64 forward, an fp32 cache's to the
+    fp32 bounds, a bf16 cache's to a rounding step of K and V (2^-8 of each, and as much again by the scores)."""
+    m = Model(SHAPES[64], kv_fp32=kv_fp32, **FEATURES["all"])
+    x, step = torch.randn(4, 40, 256), torch.randn(4, 1, 256)
+    m.of = {b: IDS[b] for b in range(4)}
+    want = [np.stack([m.forward(b, z[b]) for b in range(4)]) for z in (x, step)]
+    for groups in ([[0, 1]], [[0], [1]], [[1], [0]]):
+        with harness.compute_stream() as cs:
+            h = P.stage_init(m.config(compute_stream=cs.handle))
+            try:
+                m.load(h)
+                for b in range(4):
+                    P.stage_set_adapter(h, b // 2, b % 2, IDS[b])
+                for call, z, ref in ((P.stage_prefill, x, want[0]), (P.stage_decode, step, want[1])):
+                    got = torch.empty(z.shape)
+                    for g in groups:
+                        at = [2 * mb + b for mb in g for b in range(2)]
+                        z_in = z[at].cuda()
+                        z_out = torch.empty_like(z_in)
+                        call(h, g, 2, z.shape[1], z_in, z_out) if call is P.stage_prefill else call(h, g, 2, z_in, z_out)
+                        P.stage_sync(h)
+                        got[at] = z_out.cpu()
+                    if kv_fp32:
+                        _check([got], [ref])
+                    else:
+                        assert harness.fp32_errors(got.numpy(), ref)[0] < 2 ** -7
+            finally:
+                P.stage_destroy(h)
