@@ -121,6 +121,10 @@ __device__ __forceinline__ f32x4_t whole_sums(const AdapterArgs &a, int row, int
         float x[8], y[8];
         if (a.x_pair) load8_pair(a.x, (size_t)row * a.x_ld + pair_at(k), x);
         else load8(a.x, (size_t)row * a.x_ld + k, STAGE_F32, x);
+        bool nan = false;   // (with one the rest does not matter)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) nan |= x[j] != x[j];
+        if (nan) return f32x4_t{NAN, NAN, NAN, NAN};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             load8(w, (size_t)i * a.k + k, STAGE_BF16, y);
@@ -271,21 +275,24 @@ __device__ __forceinline__ u32x4 cut_ranks(u32x4 v, int j0, int rank) {
     return v;
 }
 
-// A column of a row's B t, likewise.
-__device__ __forceinline__ float whole_output(const AdapterArgs &a, int slices, int row, int id, int col) {
+// 16 columns of a row's B t, likewise, from column `col` on.
+__device__ __forceinline__ void whole_outputs(const AdapterArgs &a, int slices, int row, int id, int col, f32x4_t (&v)[4]) {
     asm volatile("" : "+v"(id), "+v"(row));
     const int rank = rank_of(a, id);
     const float scale = a.scales ? a.scales[id] : 1.f;
-    const uint16_t *const w = a.b + ((size_t)id * a.n + col) * a.max_rank;
-    float v = 0.f;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) v[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int j = 0; j < rank; ++j) {
         float t = 0.f;
 #pragma unroll 1
         for (int s = 0; s < slices; ++s) t += a.part[((size_t)s * a.rows + row) * a.max_rank + j];
-        v = fmaf(t * scale, __uint_as_float((uint32_t)w[j] << 16), v);
+        t *= scale;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)   // (columns past the last: that one)
+            v[i / 4][i % 4] = fmaf(t, __uint_as_float((uint32_t)a.b[((size_t)id * a.n + min(col + i, a.n - 1)) * a.max_rank + j] << 16), v[i / 4][i % 4]);
+        if (t != t) break;
     }
-    return v;
 }
 
 // At most n memory operations of this wavefront still under way (fewer where n is between two of the counts).
@@ -538,15 +545,8 @@ __global__ __launch_bounds__(256, T_STEPS * kStep <= kRanks ? 3 : 1) void adapte
             if (any) stores = E;
             const int c0 = kCols * p0.nb + 16 * lq;
             if (write && c0 < a.n) {
-                if (__builtin_expect((t.id >= 0) & (not_finite(sum[0]) | not_finite(sum[1]) | not_finite(sum[2]) | not_finite(sum[3])), 0)) {
-#pragma unroll 1
-                    for (int c = 0; c < 16 && c0 + c < a.n; ++c) {
-                        const float v = whole_output(a, pl.slices, row, t.id, c0 + c);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (i == c && !(fabsf(sum[i / 4][i % 4]) < INFINITY)) sum[i / 4][i % 4] = v;
-                    }
-                }
+                if (__builtin_expect((t.id >= 0) & (not_finite(sum[0]) | not_finite(sum[1]) | not_finite(sum[2]) | not_finite(sum[3])), 0))
+                    whole_outputs(a, pl.slices, row, t.id, c0, sum);
                 const uint32_t from = y_ring + p0.slot * L::Y_STAGE + l16 * (16 * YCH);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {   // eight columns

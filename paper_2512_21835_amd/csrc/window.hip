@@ -121,10 +121,12 @@ struct Columns {
         const size_t head = (size_t)kPage * D;
         f32x4_t o2[D / 16];
         float m2 = -INFINITY, l2 = 0.f;
+        const bool mine = lanes >> (lane & 15) & 0x0001000100010001ull;
+        bool done = !mine;   // (a score that is NaN makes the column NaN, whatever follows)
 #pragma unroll
         for (int b = 0; b < D / 16; ++b) o2[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-        for (int u = beg * kPage; u < end * kPage; ++u) {
+        for (int u = beg * kPage; u < end * kPage && __builtin_amdgcn_ballot_w64(!done) != 0; ++u) {
             const int page = sp.page(u / kPage), key = page * kPage + u % kPage, block = ((const_ints)(uintptr_t)table)[page];
             if ((unsigned)block >= (unsigned)a.rows.n_blocks) continue;
             const size_t k = (size_t)block * 2 * a.n_kv_heads * head + u % kPage * D + 4 * lq, v = k + a.n_kv_heads * head;
@@ -153,8 +155,10 @@ struct Columns {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o2[b][i] = o2[b][i] * alpha + (seen ? w * x[i] : 0.f);
             }
+            done |= w != w;
+            l2 = done ? NAN : l2;
         }
-        if (lanes >> (lane & 15) & 0x0001000100010001ull) {
+        if (mine) {
             m = m2 + kRoomBits;
             l = l2;
 #pragma unroll
@@ -894,10 +898,11 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void window_tiles(WindowAr
     if (!same) store();
     const bool bad = t < rows && not_finite(l, o);
     if (lane == 0) flags[wave] = 0;
-    if (odd | bad) flags[wave] = 1;
+    if (bad) flags[wave] = 1;
+    if (odd) flags[wave] = 2;
     __syncthreads();
-    const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
-    if (__builtin_expect(any, 0)) by_keys<D, TYPE, STAGE_BF16>(a, rb, g, q_at, pos, bad, o, l);
+    const int any = max(max(flags[0], flags[1]), max(flags[2], flags[3]));
+    if (__builtin_expect(any, 0)) by_keys<D, TYPE, STAGE_BF16>(a, rb, g, q_at, pos, bad, any > 1, o, l);
     if (__builtin_expect(any | same, 0)) store();
 }
 

@@ -332,10 +332,11 @@ __global__ __launch_bounds__(256, 1) void window_tiles_f32(WindowArgs a, int log
     if (!same) store();
     const bool bad = row < rows && not_finite(l, o);
     if (lane == 0) flags[wave] = 0;
-    if (odd | bad) flags[wave] = 1;
+    if (bad) flags[wave] = 1;
+    if (odd) flags[wave] = 2;
     __syncthreads();
-    const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
-    if (__builtin_expect(any, 0)) by_keys<D, TYPE, STAGE_F32>(a, rb, g, q_at, pos, bad, o, l);
+    const int any = max(max(flags[0], flags[1]), max(flags[2], flags[3]));
+    if (__builtin_expect(any, 0)) by_keys<D, TYPE, STAGE_F32>(a, rb, g, q_at, pos, bad, any > 1, o, l);
     if (__builtin_expect(any | same, 0)) store();
 }
 

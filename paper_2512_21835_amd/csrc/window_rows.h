@@ -216,23 +216,24 @@ __device__ __forceinline__ bool not_finite(float l, const f32x16_t (&o)[NB]) {
 // The column of a lane (and of lane ^ 32: d 32 c + 8 j + 4 (lane / 32) + i in o[c][4 j + i]) key by key in fp32, where terms
 // cannot give it: an infinity has none, and 0 x inf in the matrix instructions meets columns that do not see it.  Columns
 // marked `again` (sums that pass the largest number among them: scaled by kRoom, they do not), and those that see a K or V
-// that is not finite, or too large to be rounded to bf16; others keep o and l.
+// that is not finite, or too large to be rounded to bf16 (looked for if some are there); others keep o and l.
 template <int D, int TYPE, int KV_TYPE>
-__device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb, int g, size_t q_at, int pos, bool again, f32x16_t (&o)[D / 32], float &l) {
+__device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb, int g, size_t q_at, int pos, bool again, bool some,
+                                        f32x16_t (&o)[D / 32], float &l) {
     const int half = __lane_id() >> 5;
     const size_t head = (size_t)kPage * D;
-    auto each_key = [&](auto use) {   // use(key, place of K, place of V), the lane's half of them
+    auto each_key = [&](bool all, auto use) {   // until !use(key, place of K, place of V), the lane's half of them
 #pragma unroll 1
-        for (int i = 0; i < rb.n_tiles * kTileKeys; ++i) {
+        for (int i = 0; all && i < rb.n_tiles * kTileKeys; ++i) {
             const int key = rb.tile_at(i / kTileKeys) * kTileKeys + i % kTileKeys;
             if (key / kPage > rb.last_page) continue;
             const int b = ((const_ints)(uintptr_t)rb.seq.table)[key / kPage];
             if ((unsigned)b >= (unsigned)a.rows.n_blocks) continue;
             const size_t k = ((size_t)b * 2 * a.n_kv_heads + g) * head + key % kPage * D;
-            use(key, k + 8 * half, k + a.n_kv_heads * head + 4 * half);
+            all = use(key, k + 8 * half, k + a.n_kv_heads * head + 4 * half);
         }
     };
-    each_key([&](int key, size_t k, size_t v) {
+    each_key(some, [&](int key, size_t k, size_t v) {
         uint32_t most = 0;
         float x[4];
 #pragma unroll 1
@@ -247,15 +248,17 @@ __device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb,
                 for (int e = 0; e < 4; ++e) most = max(most, size_bits(x[e]));
             }
         again |= sees(a, pos, key) & (most > size_bits(kMaxBf16));
+        return true;
     });
     again = __shfl_xor((int)again, 32) | (int)again;
     float m = -INFINITY;
+    bool done = !again;   // (a score that is NaN makes the column NaN, whatever follows)
     l = again ? 0.f : l;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] = again ? 0.f : o[b][i];
-    each_key([&](int key, size_t k, size_t v) {
+    each_key(true, [&](int key, size_t k, size_t v) {
         float w = 0.f;
 #pragma unroll 1
         for (int kk = 0; kk < D / 16; ++kk) {
@@ -285,6 +288,9 @@ __device__ __forceinline__ void by_keys(const WindowArgs &a, const RowBlock &rb,
                 for (int e = 0; e < 4; ++e) o[c][4 * j + e] = o[c][4 * j + e] * alpha + (seen ? w * x[e] : 0.f);
                 __builtin_amdgcn_sched_barrier(0);   // (registers)
             }
+        done |= w != w;
+        l = done & again ? NAN : l;
+        return __builtin_amdgcn_ballot_w64(!done) != 0;
     });
 }
 // With a turn before and a turn behind each run.

@@ -235,3 +235,33 @@ def test_adapters_of_many_ranks_and_slices(rows, k, n, adapters, rank, act):
     _check_adapter(_adapter_case(rows, k, n, adapters, rank, act, ids), _run_adapter(_adapter_case(rows, k, n, adapters, rank, act, ids)))
     c = _adapter_case(rows, k, n, adapters, rank, act, ids, ranks)
     _check_adapter(c, _run_adapter(c))
+
+
+@pytest.mark.parametrize("act,cache", [("fp32", "bf16"), ("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "fp32")])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE + [([20, 1, 5], [3000, 90, 1000], 8, 2)])
+def test_a_query_that_is_nan_stays_with_its_row(rows, held, hq, hkv, cache, act):
+    b, q, out = c = _window_case(rows, held, hq, hkv, 64, act, cache)
+    for window, sinks in ((0, 0), (1500, 2)):
+        want = _run_window(c, window, sinks)
+        at = len(q) - 2
+        old = q[at].clone()
+        q[at, :, 3::9] = float("nan")
+        got = _run_window(c, window, sinks)
+        assert bool(torch.isnan(got[at]).all())
+        q[at] = old
+        got[at] = want[at]
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,k,n,adapters,rank", ADAPTERS)
+def test_an_input_that_is_nan_stays_with_its_row(rows, k, n, adapters, rank, act):
+    c = _adapter_case(rows, k, n, adapters, rank, act, [i % adapters for i in range(rows)])
+    want = _run_adapter(c)
+    for at in (slice(None), slice(k - 1, None)):
+        bad = c[0].clone()
+        bad[1, at] = float("nan")
+        got = _run_adapter((bad, *c[1:]))
+        assert bool(torch.isnan(got[1]).all())
+        got[1] = want[1]
+        assert torch.equal(got, want)
