@@ -248,6 +248,10 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a, Adapte
         if (wave == (turn & 3) && t.id == it.id && j0 < a.max_rank) {
             const f32x4_t *const p = &sums[turn & 1][0][lane];
             f32x4_t v = ((p[0] + p[64]) + p[128]) + p[192];
+            if constexpr (TERMS > 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = j0 + i < t.rank ? v[i] : 0.f;   // (past the rank A holds anything)
+            }
             if (__builtin_expect(TERMS > 1 && not_finite(v), 0)) v = whole_sums(a, row0 + l16, it.id, j0, 4 * slice * pl.wave_k, 4 * pl.wave_k);
             *reinterpret_cast<f32x4_t *>(a.part + ((size_t)slice * a.rows + row0 + l16) * a.max_rank + j0) = v;
         }

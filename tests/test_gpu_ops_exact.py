@@ -265,3 +265,14 @@ def test_an_input_that_is_nan_stays_with_its_row(rows, k, n, adapters, rank, act
         assert bool(torch.isnan(got[1]).all())
         got[1] = want[1]
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("act", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,k,n,adapters,rank", ADAPTERS)
+def test_adapters_hold_anything_past_their_ranks(rows, k, n, adapters, rank, act):
+    ranks = [max(1, rank // 2 - 3 * i) for i in range(adapters)]
+    c = _adapter_case(rows, k, n, adapters, rank, act, [i % adapters for i in range(rows)], ranks)
+    want = _run_adapter(c)
+    for i, r in enumerate(ranks):
+        c[2][i, r:], c[3][i, :, r:] = float("nan"), float("inf")
+    assert torch.equal(_run_adapter(c), want)
