@@ -160,7 +160,8 @@ typedef struct {
        head_norm 1: query and key heads are normalised before their rotation, x / sqrt(mean(x^2) + rms_eps) * gain,
        by gains of head_dim elements that all query and all key heads share (stage_layer_weights.gq, gk).
        window > 0: a token attends to the last `window` tokens (itself included) and to the sequence's first `sinks`;
-       the cache keeps them all.  sinks needs a window.
+       the cache keeps them all.  sinks needs a window.  The order in which a row's keys are added up, and so its last
+       bits, then go by the call's sizes (rows, sequences, longest length).
        max_adapters > 0: up to that many low-rank adapters (stage_load_adapter, stage_set_adapter), of rank up to
        adapter_rank, a multiple of 4 of at most STAGE_OPS_MAX_RANK (include/stage_ops.h). */
     int32_t head_norm;

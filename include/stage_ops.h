@@ -107,9 +107,9 @@ int stage_norm_rope_append(const stage_append_args *a, void *stream);
    activations the probabilities, and the values of an fp32 cache, may be held to 2^-16 of their sizes.  Nothing of
    a place that a row does not see reaches its result, infinities and NaN among it; those that it sees give what they give
    in the formula.  Tokens in blocks whose id is not one of the pool's are not seen; a row that sees none (its position is
-   negative, say) becomes 0.  out may be q itself, with the same stride; else they share no element.  The order in which a
-   row's keys are added up goes by the call's sizes (rows, sequences, longest length): the same call gives the same bits,
-   the same row in another call the same to rounding. */
+   negative, say), or none of a score above -inf, becomes 0.  out may be q itself, with the same stride; else they share
+   no element.  The order in which a row's keys are added up goes by the call's sizes (rows, sequences, longest length): the
+   same call gives the same bits, the same row in another call the same to rounding. */
 typedef struct {
     int32_t device;
     stage_batch batch;

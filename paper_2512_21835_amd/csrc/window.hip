@@ -7,7 +7,7 @@
 // window_split: rows in blocks of 16 columns (G query heads of a KV head x 16 / G positions), the pages cut
 // over workgroups and their wavefronts, states joined at the end (window_merge where the workgroups are several).
 // Bound by the cache's bytes: 64 single tokens of 64 heads over up to 4096 bf16 tokens each (8 KV heads, 727 MB)
-// 140 us, 5.2 TB/s; a page costs a wavefront 1.2 us of dependent reads, products and softmax (fp32: 2.3), which
+// 138 us, 5.3 TB/s; a page costs a wavefront 1.2 us of dependent reads, products and softmax (fp32: 2.3), which
 // is what shorter lists take (16 tokens of 32 heads over up to 1024 fp32 tokens, 83 MB: 38 us).
 //
 // window_tiles: prompts over a bf16 cache (over an fp32 cache: window_f32.hip).
@@ -562,11 +562,11 @@ hipError_t launch_split(const WindowArgs &a, hipStream_t st) {
 // term of q) are laid between the MFMAs by hand.  Fragments are in registers half a turn before their MFMAs: V's are
 // read under the scores, K's of the tile behind under the values.
 //
-// 4 x 2048 bf16 rows of 64 heads, window 1024: 359 us, 0.86 PFLOP/s of issued products (1.5 times the formula's, for the
+// 4 x 2048 bf16 rows of 64 heads, window 1024: 357 us, 0.87 PFLOP/s of issued products (1.5 times the formula's, for the
 // probabilities' second term; with one term, the output off by its own rounding once more, 286 us).  What is not loop is
 // beginning (block search, page ids, first tiles: 3 to 4 us a workgroup), end, and the halves of tiles outside the window.
 // 256 columns a workgroup (each wavefront 64) are slower: one wavefront per SIMD hides less than two.  fp32 rows issue three
-// times the products: 12 prompts of up to 500 rows, window 512, 123 us.
+// times the products: 12 prompts of up to 500 rows, window 512, 126 us.
 template <int D>
 struct TileLds {
     static constexpr int KEYS = 32, ROW = 2 * D, HALF = KEYS * ROW, BYTES = 2 * HALF, CH = ROW / 16;

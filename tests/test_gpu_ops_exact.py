@@ -276,3 +276,14 @@ def test_adapters_hold_anything_past_their_ranks(rows, k, n, adapters, rank, act
     for i, r in enumerate(ranks):
         c[2][i, r:], c[3][i, :, r:] = float("nan"), float("inf")
     assert torch.equal(_run_adapter(c), want)
+
+
+@pytest.mark.parametrize("act,cache", [("fp32", "bf16"), ("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "fp32")])
+@pytest.mark.parametrize("rows,held,hq,hkv", F32_CACHE)
+def test_a_row_of_scores_of_minus_infinity_becomes_0(rows, held, hq, hkv, cache, act):
+    b, q, out = c = _window_case(rows, held, hq, hkv, 64, act, cache)
+    q[..., 9] = q[..., 9].abs() + 0.1
+    block = b.table[0, :(b.lengths[0] + 15) // 16].long()
+    b.pool[block, 0, :, :, 9] = -float("inf")
+    got = _run_window(c, 40, 2)
+    assert not bool(got[:rows[0]].any()) and bool(torch.isfinite(got).all()) and bool(got[rows[0]:].any(-1).all())
