@@ -18,6 +18,7 @@
 #include "lanes.h"
 #include "lds_dma.h"
 #include "ops_kernels.h"
+#include "rows8.h"
 #include "stage_ops.h"
 
 namespace stg {
@@ -25,7 +26,6 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) u32x4 *lds16;
 
 constexpr int kTile = 16;     // rows of a tile
@@ -41,18 +41,6 @@ __device__ __forceinline__ void load8(const void *p, size_t e, int type, float v
         const bf16x8_t b = *reinterpret_cast<const bf16x8_t *>(static_cast<const uint16_t *>(p) + e);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (float)b[j];
-    }
-}
-__device__ __forceinline__ void store8(void *p, size_t e, int type, const float v[8]) {
-    if (type == STAGE_F32) {
-        float4 *f = reinterpret_cast<float4 *>(static_cast<float *>(p) + e);
-        f[0] = make_float4(v[0], v[1], v[2], v[3]);
-        f[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-        bf16x8_t b;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = (__bf16)v[j];
-        *reinterpret_cast<bf16x8_t *>(static_cast<uint16_t *>(p) + e) = b;
     }
 }
 // Eight elements of a hi/lo pair, whose sum is exact.
